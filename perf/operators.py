@@ -181,7 +181,7 @@ def _plain(s):
         h, rstd = _plain_norm(s["x"], s["residual"], s["weight"])
         u = h.float() * s["weight"].float()
         top = u.abs().amax(1)
-        codes = torch.round(u * (127.0 / top)[:, None])
+        codes = torch.round(u * torch.div(torch.full_like(top, 127.0), top)[:, None])
         return {"h": h, "values": codes * (top * rstd / 127.0)[:, None]}
     if op == "norm":
         h, rstd = _plain_norm(s["x"], s["residual"], s["weight"])
