@@ -1,0 +1,400 @@
+// Embedding lookup with scaling, and its gradient.
+//
+// Lookup: bound by memory, one read and one write of a row's bytes; nothing is computed but the scale.
+//
+// Gradient: the tokens are sorted by id (stable, so that a row's tokens keep their order), then summed in chunks of CHUNK sorted
+// places.  A row whose tokens lie within a chunk is finished there; one that runs on leaves a partial sum in each chunk, and the
+// chunk that it began in joins them in order.  No atomics on sums: results do not depend on the order of workgroups.  A
+// frequent token (8 % of a text's tokens are one word) is so spread over many workgroups.
+// Bound: the zeros of the rows without a token, V * D values, are most of what is written.
+#include <algorithm>
+
+#include "simple_vocabdev.hpp"
+
+namespace simple {
+namespace embed {
+
+using namespace vocab;
+
+constexpr int WG = 256;
+constexpr int RD = 4;              // rows in flight per thread of the lookup
+constexpr int TILE = 2048;         // tokens a workgroup of the sort
+constexpr int BITS = 9, BINS = 1 << BITS;
+constexpr int CHUNK = 32;          // sorted places a workgroup of the sums
+constexpr int ROUNDS = TILE / WG;  // a wave's tokens, 64 at a time
+
+// ---- lookup ----
+template <typename T, int VEC>
+__global__ __launch_bounds__(WG) void lookup_kernel(const int32_t* ids, const T* table, int64_t table_stride, int64_t n, int64_t V, int64_t D,
+                                                    float scale, T* out, int64_t out_stride) {
+  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+  if (c >= D) return;
+  const int64_t r0 = (int64_t)blockIdx.x * (blockDim.y * RD) + threadIdx.y;
+  float v[RD][VEC];
+#pragma unroll
+  for (int k = 0; k < RD; ++k) {
+    const int64_t r = r0 + k * blockDim.y;
+    const int id = r < n ? ids[r] : -1;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) v[k][j] = 0.f;
+    if (id >= 0 && id < V) load<T, VEC>(table + id * table_stride + c, v[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < RD; ++k) {
+    const int64_t r = r0 + k * blockDim.y;
+    if (r >= n) return;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) v[k][j] *= scale;
+    store<T, VEC>(out + r * out_stride + c, v[k]);
+  }
+}
+
+// ---- zeros ----
+struct Fill {
+  unsigned char* p;
+  int64_t rows, row_bytes, stride_bytes;
+};
+// Workgroup `at` of `n`: its share of the rows, in pieces of 16 bytes where the address allows it, else of 2.
+__device__ __forceinline__ void fill_share(const Fill& f, int64_t at, int64_t n) {
+  typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+  const bool whole = f.row_bytes == f.stride_bytes;  // one long row
+  const int64_t rows = whole ? 1 : f.rows, bytes = whole ? f.rows * f.row_bytes : f.row_bytes;
+  for (int64_t r = whole ? 0 : at; r < rows; r += whole ? 1 : n) {
+    unsigned char* p = f.p + r * f.stride_bytes;
+    const int64_t head = min(bytes, (int64_t)((16u - (uint32_t)(uintptr_t)p) & 15u)), body = (bytes - head) / 16;
+    const int64_t first = whole ? at * WG : 0, step = whole ? n * WG : WG;
+    for (int64_t i = first + threadIdx.x; i < body; i += step) *reinterpret_cast<v4u*>(p + head + 16 * i) = v4u{0u, 0u, 0u, 0u};
+    if (!whole || at == 0) {
+      for (int64_t i = 2 * threadIdx.x; i < head; i += 2 * WG) *reinterpret_cast<uint16_t*>(p + i) = 0;
+      for (int64_t i = head + 16 * body + 2 * threadIdx.x; i < bytes; i += 2 * WG) *reinterpret_cast<uint16_t*>(p + i) = 0;
+    }
+  }
+}
+
+// ---- sort: stable, BITS bits of the id a pass, from the lowest ----
+struct Sort {
+  const int32_t *key_in, *pos_in;  // pos_in null: first pass, the tokens in their own order
+  int32_t *key_out, *pos_out;
+  int32_t* counts;                 // [tiles][BINS]
+  int64_t n, V;
+  int tiles, shift;
+};
+// An id outside the vocabulary sorts behind all others, as V.
+__device__ __forceinline__ int32_t key_of(const Sort& s, int64_t i) {
+  const int32_t k = s.key_in[i];
+  return (k < 0 || k >= s.V) ? (int32_t)s.V : k;
+}
+
+__global__ __launch_bounds__(WG) void count_kernel(Sort s, Fill f) {
+  if ((int)blockIdx.x >= s.tiles) { fill_share(f, (int)blockIdx.x - s.tiles, (int)gridDim.x - s.tiles); return; }
+  __shared__ int32_t cnt[BINS];
+  for (int i = threadIdx.x; i < BINS; i += WG) cnt[i] = 0;
+  __syncthreads();
+  const int64_t t0 = (int64_t)blockIdx.x * TILE;
+  for (int k = 0; k < ROUNDS; ++k) {
+    const int64_t i = t0 + k * WG + threadIdx.x;
+    if (i < s.n) atomicAdd(&cnt[((uint32_t)key_of(s, i) >> s.shift) & (BINS - 1)], 1);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < BINS; i += WG) s.counts[(int64_t)blockIdx.x * BINS + i] = cnt[i];
+}
+
+// A tile's tokens go to their places: behind all tokens of lower digits, those of the same digit in earlier tiles, in earlier waves
+// of the tile, in earlier rounds of the wave and in lower lanes.
+__global__ __launch_bounds__(WG) void place_kernel(Sort s, Fill f) {
+  if ((int)blockIdx.x >= s.tiles) { fill_share(f, (int)blockIdx.x - s.tiles, (int)gridDim.x - s.tiles); return; }
+  constexpr int NW = WG / 64;
+  __shared__ int32_t cnt[NW][BINS];
+  __shared__ int32_t scan[NW];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  for (int i = tid; i < NW * BINS; i += WG) (&cnt[0][0])[i] = 0;
+  // counts of the tiles ahead, and of all
+  int32_t ahead[2] = {0, 0}, all[2] = {0, 0};
+  if (s.tiles > 1) {
+#pragma unroll 4
+    for (int t = 0; t < s.tiles; ++t) {
+      const int2 c = *reinterpret_cast<const int2*>(s.counts + (int64_t)t * BINS + 2 * tid);
+      all[0] += c.x; all[1] += c.y;
+      if (t < (int)blockIdx.x) { ahead[0] += c.x; ahead[1] += c.y; }
+    }
+  }
+  __syncthreads();
+  const int64_t w0 = (int64_t)blockIdx.x * TILE + wave * (ROUNDS * 64);
+  int32_t key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
+#pragma unroll
+  for (int k = 0; k < ROUNDS; ++k) {
+    const int64_t i = w0 + k * 64 + lane;
+    key[k] = i < s.n ? key_of(s, i) : 0;
+    pos[k] = i < s.n ? (s.pos_in ? s.pos_in[i] : (int32_t)i) : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < ROUNDS; ++k) {
+    const bool in = w0 + k * 64 + lane < s.n;
+    const uint32_t d = ((uint32_t)key[k] >> s.shift) & (BINS - 1);
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < BITS; ++b) {
+      const uint64_t set = __ballot((d >> b) & 1u);
+      same &= ((d >> b) & 1u) ? set : ~set;
+    }
+    const int first = in ? __ffsll((unsigned long long)same) - 1 : lane;
+    int32_t old = 0;
+    if (in && lane == first) old = atomicAdd(&cnt[wave][d], (int32_t)__popcll(same));
+    rank[k] = __shfl(old, first, 64) + (int32_t)__popcll(same & ((1ull << lane) - 1ull));
+  }
+  __syncthreads();
+  // first place of each digit for this tile, then for each of its waves
+  int32_t own[2] = {0, 0};
+#pragma unroll
+  for (int w = 0; w < NW; ++w) { own[0] += cnt[w][2 * tid]; own[1] += cnt[w][2 * tid + 1]; }
+  if (s.tiles == 1) { all[0] = own[0]; all[1] = own[1]; }
+  int32_t pre = all[0] + all[1];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int32_t up = __shfl_up(pre, o, 64);
+    if (lane >= o) pre += up;
+  }
+  if (lane == 63) scan[wave] = pre;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) pre += scan[w];
+  int32_t base[2] = {pre - all[0] - all[1] + ahead[0], pre - all[1] + ahead[1]};
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const int32_t c0 = cnt[w][2 * tid], c1 = cnt[w][2 * tid + 1];
+    cnt[w][2 * tid] = base[0]; cnt[w][2 * tid + 1] = base[1];
+    base[0] += c0; base[1] += c1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < ROUNDS; ++k) {
+    if (w0 + k * 64 + lane < s.n) {
+      const int32_t to = cnt[wave][((uint32_t)key[k] >> s.shift) & (BINS - 1)] + rank[k];
+      s.key_out[to] = key[k];
+      s.pos_out[to] = pos[k];
+    }
+  }
+}
+
+// ---- sums ----
+struct Sums {
+  const int32_t *key, *pos;  // sorted
+  const void* dout;
+  int64_t dout_stride, n, V, D;
+  float scale;
+  void* dtable;
+  int64_t dtable_stride;
+  int accumulate;
+  float* partial;  // [chunks][2][D]: of the row that the chunk begins inside, and of the one that it ends inside
+};
+
+template <typename TO, int VEC> __device__ __forceinline__ void finish(const Sums& s, int32_t id, int64_t c, float (&acc)[VEC]) {
+  TO* to = (TO*)s.dtable + id * s.dtable_stride + c;
+  float v[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) v[j] = 0.f;
+  if (s.accumulate) load<TO, VEC>(to, v);
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) v[j] = fmaf(acc[j], s.scale, v[j]);
+  store<TO, VEC>(to, v);
+}
+
+template <typename T, typename TO, int VEC>
+__global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
+  __shared__ int32_t key[CHUNK + 2], pos[CHUNK];
+  const int64_t chunk = blockIdx.x, s0 = chunk * CHUNK;
+  const int m = (int)min((int64_t)CHUNK, s.n - s0);
+  for (int i = threadIdx.x; i < CHUNK + 2; i += blockDim.x) {
+    const int64_t at = s0 + i - 1;
+    key[i] = at >= 0 && at < s.n ? s.key[at] : -1;
+    if (i < m) pos[i] = s.pos[s0 + i];
+  }
+  __syncthreads();
+  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+  if (c >= s.D || key[1] >= s.V) return;
+  const T* d = (const T*)s.dout + c;
+  float acc[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
+  bool inside = key[0] == key[1];  // the row began in an earlier chunk
+  constexpr int AHEAD = 8;
+  static_assert(CHUNK % AHEAD == 0, "loads in flight");
+  for (int i0 = 0; i0 < m; i0 += AHEAD) {
+    float v[AHEAD][VEC];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (i0 + u < m && key[1 + i0 + u] < s.V) load<T, VEC>(d + pos[i0 + u] * s.dout_stride, v[u]);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int i = i0 + u;
+      if (i >= m || key[1 + i] >= s.V) break;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
+      if (key[1 + i] != key[2 + i]) {  // the row's last token
+        if (inside) store<float, VEC>(s.partial + 2 * chunk * s.D + c, acc);
+        else finish<TO, VEC>(s, key[1 + i], c, acc);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
+        inside = false;
+      } else if (i == m - 1) {         // the row runs on
+        store<float, VEC>(s.partial + (2 * chunk + (inside ? 0 : 1)) * s.D + c, acc);
+      }
+    }
+  }
+}
+
+// The row that chunk blockIdx.x ends inside, if it began there: its partial sums, in order.
+template <typename TO, int VEC>
+__global__ __launch_bounds__(WG) void join_kernel(Sums s) {
+  const int64_t chunk = blockIdx.x, e = (chunk + 1) * CHUNK;  // (the grid leaves the last chunk out)
+  const int32_t id = s.key[e - 1];
+  if (id >= s.V || s.key[e] != id) return;
+  if (s.key[chunk * CHUNK] == id && chunk > 0 && s.key[chunk * CHUNK - 1] == id) return;
+  // the first chunk that the row does not run out of
+  __shared__ int32_t found;
+  int64_t end = chunk + 1;
+  for (bool more = true; more; ) {
+    if (threadIdx.x == 0) found = (int32_t)blockDim.x;
+    __syncthreads();
+    const int64_t after = (end + threadIdx.x + 1) * CHUNK;  // the place behind chunk end + threadIdx.x
+    if (after >= s.n || s.key[after] != id) atomicMin(&found, (int32_t)threadIdx.x);
+    __syncthreads();
+    end += found;
+    more = found == (int32_t)blockDim.x;
+    __syncthreads();
+  }
+  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+  if (c >= s.D) return;
+  float acc[VEC];
+  load<float, VEC>(s.partial + (2 * chunk + 1) * s.D + c, acc);
+  const float* p = s.partial + 2 * (chunk + 1) * s.D + c;
+  const int64_t m = end - chunk;
+  constexpr int AHEAD = 8;
+  for (int64_t k = 0; k < m; k += AHEAD) {
+    float v[AHEAD][VEC];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (k + u < m) load<float, VEC>(p + 2 * (k + u) * s.D, v[u]);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (k + u < m) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
+      }
+  }
+  finish<TO, VEC>(s, id, c, acc);
+}
+
+struct Layout { int64_t key[2], pos[2], counts, partial, total; int tiles, passes; };
+Layout layout(int64_t T, int64_t V, int64_t D) {
+  Layout L{};
+  auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
+  L.tiles = (int)ceil_div(T, TILE);
+  L.passes = 1;
+  while ((V >> (L.passes * BITS)) != 0) ++L.passes;
+  for (int i = 0; i < 2; ++i) { L.key[i] = take(T * 4); L.pos[i] = take(T * 4); }
+  L.counts = take((int64_t)L.tiles * BINS * 4);
+  L.partial = take(ceil_div(T, CHUNK) * 2 * D * 4);
+  return L;
+}
+
+}  // namespace embed
+}  // namespace simple
+
+using namespace simple::embed;
+
+namespace {
+int check_sizes(int64_t T, int64_t V, int64_t D, int dtype) {
+  if (T < 0 || V <= 0 || D <= 0 || !good_type(dtype)) return SIMPLE_EINVAL;
+  if (T > (int64_t)0x7FFFFFFF || V >= (int64_t)0x7FFFFFFF || D > ((int64_t)1 << 22)) return SIMPLE_ECAPACITY;
+  return SIMPLE_OK;
+}
+int shape_of(int64_t units) {  // threads along a row
+  int x = 8;
+  while (x < WG && x < units) x *= 2;
+  return x;
+}
+}  // namespace
+
+extern "C" int simple_embed(const int32_t* ids_dev, const void* table_dev, int64_t table_stride, int64_t T, int64_t V, int64_t D, int dtype,
+                            float scale, void* out_dev, int64_t out_stride, void* hip_stream) {
+  const int rc = check_sizes(T, V, D, dtype);
+  if (rc != SIMPLE_OK) return rc;
+  if (table_stride < D || out_stride < D) return SIMPLE_EINVAL;
+  if (T == 0) return SIMPLE_OK;
+  if (!ids_dev || !table_dev || !out_dev) return SIMPLE_EINVAL;
+  const int64_t e = type_bytes(dtype);
+  const bool wide = D % (16 / e) == 0 && rows_aligned(table_dev, table_stride, e, 16) && rows_aligned(out_dev, out_stride, e, 16);
+  const int64_t units = wide ? D / (16 / e) : D;
+  const int x = shape_of(units), y = WG / x;
+  const dim3 grid((unsigned)ceil_div(T, (int64_t)y * RD), (unsigned)ceil_div(units, x)), block(x, y);
+  if (grid.y > 65535) return SIMPLE_ECAPACITY;
+  auto go = [&](auto kernel, auto* type) {
+    using T_ = std::remove_pointer_t<decltype(type)>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)hip_stream, ids_dev, (const T_*)table_dev, table_stride, T, V, D, scale, (T_*)out_dev, out_stride);
+  };
+  if (dtype == SIMPLE_F32) { if (wide) go(lookup_kernel<float, 4>, (float*)0); else go(lookup_kernel<float, 1>, (float*)0); }
+  else { if (wide) go(lookup_kernel<uint16_t, 8>, (uint16_t*)0); else go(lookup_kernel<uint16_t, 1>, (uint16_t*)0); }
+  return launched();
+}
+
+extern "C" int64_t simple_embed_grad_workspace(int64_t T, int64_t V, int64_t D) {
+  const int rc = check_sizes(T, V, D, SIMPLE_F32);
+  return rc != SIMPLE_OK ? rc : layout(T, V, D).total;
+}
+
+extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, int64_t dout_stride, int64_t T, int64_t V, int64_t D, int dtype,
+                                 float scale, void* dtable_dev, int64_t dtable_stride, int table_dtype, int accumulate,
+                                 void* workspace_dev, int64_t workspace_bytes, void* hip_stream) {
+  const int rc = check_sizes(T, V, D, dtype);
+  if (rc != SIMPLE_OK) return rc;
+  if (!good_type(table_dtype) || !dtable_dev || dtable_stride < D || dout_stride < D) return SIMPLE_EINVAL;
+  if (T == 0 && accumulate) return SIMPLE_OK;
+  const Layout L = layout(T, V, D);
+  if (T > 0) {
+    if (!ids_dev || !dout_dev || !workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
+    if (workspace_bytes < L.total) return SIMPLE_ECAPACITY;
+  }
+  hipStream_t st = (hipStream_t)hip_stream;
+  unsigned char* ws = (unsigned char*)workspace_dev;
+  const int64_t eo = type_bytes(table_dtype), ei = type_bytes(dtype);
+  const Fill zeros{(unsigned char*)dtable_dev, V, D * eo, dtable_stride * eo}, nothing{};
+  // the zeros are written beside the first kernel of the sort
+  const int64_t fill_bytes = V * D * eo, fill_wgs = accumulate ? 0 : std::min<int64_t>(2048, std::max<int64_t>(1, fill_bytes / (16 * WG * 4)));
+  Sort s{ids_dev, nullptr, (int32_t*)(ws + L.key[0]), (int32_t*)(ws + L.pos[0]), (int32_t*)(ws + L.counts), T, V, L.tiles, 0};
+  int64_t fill_left = fill_wgs;
+  for (int p = 0; p < (T > 0 ? L.passes : 1); ++p) {
+    if (L.tiles > 1) {
+      hipLaunchKernelGGL(count_kernel, dim3((unsigned)(L.tiles + fill_left)), dim3(WG), 0, st, s, fill_left ? zeros : nothing);
+      fill_left = 0;
+    }
+    hipLaunchKernelGGL(place_kernel, dim3((unsigned)(L.tiles + fill_left)), dim3(WG), 0, st, s, fill_left ? zeros : nothing);
+    fill_left = 0;
+    s.key_in = s.key_out; s.pos_in = s.pos_out;
+    s.key_out = (int32_t*)(ws + L.key[(p + 1) & 1]); s.pos_out = (int32_t*)(ws + L.pos[(p + 1) & 1]);
+    s.shift += BITS;
+  }
+  if (T == 0) return launched();
+  Sums m{s.key_in, s.pos_in, dout_dev, dout_stride, T, V, D, scale, dtable_dev, dtable_stride, accumulate, (float*)(ws + L.partial)};
+  // groups of 8 bfloat16 or 4 float32, by the wider of the two types
+  const int64_t vec = dtype == SIMPLE_BF16 && table_dtype == SIMPLE_BF16 ? 8 : 4;
+  const bool wide = D % vec == 0 && rows_aligned(dout_dev, dout_stride, ei, std::min<int64_t>(16, vec * ei)) &&
+                    rows_aligned(dtable_dev, dtable_stride, eo, std::min<int64_t>(16, vec * eo));
+  const int64_t units = wide ? D / vec : D, chunks = ceil_div(T, CHUNK);
+  const int x = std::max(64, shape_of(units));
+  const dim3 grid((unsigned)chunks, (unsigned)ceil_div(units, x)), rest((unsigned)(chunks - 1), grid.y);
+  if (grid.y > 65535) return SIMPLE_ECAPACITY;
+  auto go = [&](auto sums, auto join) {
+    hipLaunchKernelGGL(sums, grid, dim3(x), 0, st, m);
+    if (chunks > 1) hipLaunchKernelGGL(join, rest, dim3(x), 0, st, m);
+  };
+  if (dtype == SIMPLE_BF16 && table_dtype == SIMPLE_BF16) {
+    if (wide) go(sums_kernel<uint16_t, uint16_t, 8>, join_kernel<uint16_t, 8>); else go(sums_kernel<uint16_t, uint16_t, 1>, join_kernel<uint16_t, 1>);
+  } else if (dtype == SIMPLE_BF16) {
+    if (wide) go(sums_kernel<uint16_t, float, 4>, join_kernel<float, 4>); else go(sums_kernel<uint16_t, float, 1>, join_kernel<float, 1>);
+  } else if (table_dtype == SIMPLE_BF16) {
+    if (wide) go(sums_kernel<float, uint16_t, 4>, join_kernel<uint16_t, 4>); else go(sums_kernel<float, uint16_t, 1>, join_kernel<uint16_t, 1>);
+  } else {
+    if (wide) go(sums_kernel<float, float, 4>, join_kernel<float, 4>); else go(sums_kernel<float, float, 1>, join_kernel<float, 1>);
+  }
+  return launched();
+}

@@ -1,0 +1,49 @@
+// What the kernels around the vocabulary matrices share: bfloat16 <-> float32, groups of consecutive elements as one load or
+// store, argument checks.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "simple_vocab.h"
+
+namespace simple {
+namespace vocab {
+
+__device__ __forceinline__ float up(float v) { return v; }
+__device__ __forceinline__ float up(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+// Round to nearest even; a NaN stays one (its upper half could be all zeros behind the sign and exponent).
+__device__ __forceinline__ uint16_t to_bf16(float f) {
+  const uint32_t b = __float_as_uint(f);
+  if ((b & 0x7FFFFFFFu) > 0x7F800000u) return (uint16_t)((b >> 16) | 0x40u);
+  return (uint16_t)((b + 0x7FFFu + ((b >> 16) & 1u)) >> 16);
+}
+template <typename T> __device__ __forceinline__ T down(float f);
+template <> __device__ __forceinline__ float down<float>(float f) { return f; }
+template <> __device__ __forceinline__ uint16_t down<uint16_t>(float f) { return to_bf16(f); }
+
+// VEC consecutive elements of T, aligned to their own size together, or to 16 bytes where that is less.
+template <typename T, int VEC> struct __align__(sizeof(T) * VEC < 16 ? sizeof(T) * VEC : 16) Group { T v[VEC]; };
+template <typename T, int VEC> __device__ __forceinline__ void load(const T* p, float (&out)[VEC]) {
+  const Group<T, VEC> g = *reinterpret_cast<const Group<T, VEC>*>(p);
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) out[i] = up(g.v[i]);
+}
+template <typename T, int VEC> __device__ __forceinline__ void store(T* p, const float (&in)[VEC]) {
+  Group<T, VEC> g;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) g.v[i] = down<T>(in[i]);
+  *reinterpret_cast<Group<T, VEC>*>(p) = g;
+}
+
+// ---- host side ----
+inline bool good_type(int dtype) { return dtype == SIMPLE_F32 || dtype == SIMPLE_BF16; }
+inline int64_t type_bytes(int dtype) { return dtype == SIMPLE_F32 ? 4 : 2; }
+// Whether rows of `stride` elements of `esz` bytes that start at `p` all start at a multiple of `to` bytes.
+inline bool rows_aligned(const void* p, int64_t stride, int64_t esz, int64_t to) {
+  return p == nullptr || (((uintptr_t)p & (uintptr_t)(to - 1)) == 0 && ((stride * esz) & (to - 1)) == 0);
+}
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int launched() { return hipGetLastError() == hipSuccess ? SIMPLE_OK : SIMPLE_EDEVICE; }
+
+}  // namespace vocab
+}  // namespace simple

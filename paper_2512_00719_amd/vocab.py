@@ -1,0 +1,198 @@
+"""The operators at a model's vocabulary (``include/simple_vocab.h``) over torch device tensors.
+
+A decoding step is ``embed`` -> the model -> ``rms_norm_int8`` -> ``linear_int8`` -> a sampling call of
+``binding``; a training step ends with ``rms_norm`` -> ``linear_xent`` and begins its backward pass with
+``linear_xent_grad`` -> ``rms_norm_grad`` ... ``embed_grad``.  As in ``binding`` only arguments are checked and marshalled here:
+every step runs in the HIP kernels of the library, on the current stream, without a synchronisation.  Outputs and workspaces are allocated by torch
+where they are not passed.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import binding
+from .binding import SIMPLE_BF16, SIMPLE_F32, SIMPLE_OK, SimpleError, _addresses, _current_stream
+
+EXPORTS = ("simple_rms_norm", "simple_rms_norm_int8", "simple_quantize_rows", "simple_rms_norm_grad", "simple_rms_norm_grad_workspace",
+           "simple_embed", "simple_embed_grad", "simple_embed_grad_workspace")
+
+
+def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
+    vp, i64, f32, ci = ctypes.c_void_p, ctypes.c_int64, ctypes.c_float, ctypes.c_int
+    signatures = {
+        "simple_rms_norm": (ci, vp, i64, vp, i64, vp, i64, i64, ci, f32, vp, i64, vp, i64, vp, vp),
+        "simple_rms_norm_int8": (ci, vp, i64, vp, i64, vp, i64, i64, ci, f32, vp, i64, vp, i64, vp, vp),
+        "simple_quantize_rows": (ci, vp, i64, i64, i64, ci, vp, i64, vp, vp),
+        "simple_rms_norm_grad": (ci, vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, ci, vp, i64, vp, vp, i64, vp),
+        "simple_rms_norm_grad_workspace": (i64, i64, i64),
+        "simple_embed": (ci, vp, vp, i64, i64, i64, i64, ci, f32, vp, i64, vp),
+        "simple_embed_grad": (ci, vp, vp, i64, i64, i64, i64, ci, f32, vp, i64, ci, ci, vp, i64, vp),
+        "simple_embed_grad_workspace": (i64, i64, i64, i64),
+    }
+    assert set(signatures) == set(EXPORTS)
+    for name, (restype, *argtypes) in signatures.items():
+        f = getattr(lib, name)
+        f.restype, f.argtypes = restype, argtypes
+    return lib
+
+
+_lib = _declare(binding._lib)
+_TYPES = {torch.float32: SIMPLE_F32, torch.bfloat16: SIMPLE_BF16}
+
+
+def _check(rc: int, where: str) -> None:
+    if rc != SIMPLE_OK:
+        raise SimpleError(rc, where)
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"{name} is float32 or bfloat16, got {t.dtype}") from None
+
+
+def _tensor(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    """`t`, if it is a tensor of that kind on that device whose rows are dense (the last dimension's stride is 1)."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, others on {device}")
+    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name} has a stride of {t.stride(-1)} along its rows: 1 is wanted")
+    return t
+
+
+def _matrix(t: torch.Tensor, name: str, dtypes=(torch.float32, torch.bfloat16)) -> torch.Tensor:
+    """A [rows, values] matrix on the current GPU, the first operand of a call."""
+    if t.dim() != 2 or t.shape[1] == 0:
+        raise ValueError(f"{name} is [rows, values], got shape {tuple(t.shape)}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} is one of {dtypes}, got {t.dtype}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}: the current GPU is wanted")
+    return _tensor(t, name, t.shape, t.dtype, t.device)
+
+
+def _stride(t: Optional[torch.Tensor]) -> int:
+    """Row stride in elements.  (torch says anything for a single row.)"""
+    if t is None:
+        return 0
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _ptr(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _out(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    return torch.empty(shape, dtype=dtype, device=device) if t is None else _tensor(t, name, shape, dtype, device)
+
+
+def _workspace(nbytes: int, where: str, device: torch.device) -> torch.Tensor:
+    if nbytes < 0:
+        raise SimpleError(nbytes, where)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _norm_inputs(x, weight, residual, h):
+    _matrix(x, "x")
+    _tensor(weight, "weight", (x.shape[1],), x.dtype, x.device)
+    if residual is None:
+        if h is not None:
+            raise ValueError("h is the sum with a residual, and there is none")
+        return None
+    _tensor(residual, "residual", x.shape, x.dtype, x.device)
+    return _out(h, "h", x.shape, x.dtype, x.device)
+
+
+def rms_norm(x, weight, *, eps: float = 1e-6, residual=None, h=None, out=None, rstd=None, need_rstd: bool = False):
+    """``(y, h, rstd)``: h = x + residual (x itself without one), y = h / rms(h) * weight in x's type, rstd = 1 / rms(h) (float32 [T],
+    ``None`` unless ``need_rstd`` or a tensor for it is given).  ``h`` may be ``residual``, ``out`` may be ``x``."""
+    total = _norm_inputs(x, weight, residual, h)
+    T, D = x.shape
+    out = _out(out, "out", x.shape, x.dtype, x.device)
+    if rstd is not None or need_rstd:
+        rstd = _out(rstd, "rstd", (T,), torch.float32, x.device)
+    _check(_lib.simple_rms_norm(x.data_ptr(), _stride(x), _ptr(residual), _stride(residual), weight.data_ptr(), T, D, _TYPES[x.dtype], eps,
+                                _ptr(total), _stride(total), out.data_ptr(), _stride(out), _ptr(rstd), _current_stream()), "simple_rms_norm")
+    return out, x if total is None else total, rstd
+
+
+def rms_norm_int8(x, weight, *, eps: float = 1e-6, residual=None, h=None, codes=None, scales=None):
+    """``(codes, scales, h)``: the norm's output as int8 [T, D] and float32 [T], code * scale."""
+    total = _norm_inputs(x, weight, residual, h)
+    T, D = x.shape
+    codes = _out(codes, "codes", x.shape, torch.int8, x.device)
+    scales = _out(scales, "scales", (T,), torch.float32, x.device)
+    _check(_lib.simple_rms_norm_int8(x.data_ptr(), _stride(x), _ptr(residual), _stride(residual), weight.data_ptr(), T, D, _TYPES[x.dtype], eps,
+                                     _ptr(total), _stride(total), codes.data_ptr(), _stride(codes), scales.data_ptr(), _current_stream()),
+           "simple_rms_norm_int8")
+    return codes, scales, x if total is None else total
+
+
+def quantize_rows(x, *, codes=None, scales=None):
+    """``(codes, scales)``: rows as int8 and float32 [T], code * scale.  For the weights of ``linear_int8``, once."""
+    _matrix(x, "x")
+    T, D = x.shape
+    codes = _out(codes, "codes", x.shape, torch.int8, x.device)
+    scales = _out(scales, "scales", (T,), torch.float32, x.device)
+    _check(_lib.simple_quantize_rows(x.data_ptr(), _stride(x), T, D, _TYPES[x.dtype], codes.data_ptr(), _stride(codes), scales.data_ptr(),
+                                     _current_stream()), "simple_quantize_rows")
+    return codes, scales
+
+
+def rms_norm_grad(dy, h, weight, rstd, *, dh=None, dx=None, dweight=None):
+    """``(dx, dweight)``: gradients of ``rms_norm`` for x (and residual alike; ``dh`` is what reaches h past the norm) and for its weight
+    (float32 [D]).  ``dx`` may be ``dy`` or ``dh``."""
+    _matrix(dy, "dy")
+    T, D = dy.shape
+    _tensor(h, "h", dy.shape, dy.dtype, dy.device)
+    _tensor(weight, "weight", (D,), dy.dtype, dy.device)
+    _tensor(rstd, "rstd", (T,), torch.float32, dy.device)
+    if dh is not None:
+        _tensor(dh, "dh", dy.shape, dy.dtype, dy.device)
+    dx = _out(dx, "dx", dy.shape, dy.dtype, dy.device)
+    dweight = _out(dweight, "dweight", (D,), torch.float32, dy.device)
+    ws = _workspace(_lib.simple_rms_norm_grad_workspace(T, D), "simple_rms_norm_grad_workspace", dy.device)
+    _check(_lib.simple_rms_norm_grad(dy.data_ptr(), _stride(dy), h.data_ptr(), _stride(h), weight.data_ptr(), rstd.data_ptr(), _ptr(dh),
+                                     _stride(dh), T, D, _TYPES[dy.dtype], dx.data_ptr(), _stride(dx), dweight.data_ptr(), ws.data_ptr(),
+                                     ws.numel(), _current_stream()), "simple_rms_norm_grad")
+    return dx, dweight
+
+
+def embed(ids, table, *, scale: float = 1.0, out=None):
+    """Rows ``ids`` (int32 [T]) of ``table`` [V, D], times ``scale``.  An id outside the vocabulary gives a row of zeros."""
+    _matrix(table, "table")
+    V, D = table.shape
+    T = ids.numel()
+    _tensor(ids, "ids", (T,), torch.int32, table.device)
+    out = _out(out, "out", (T, D), table.dtype, table.device)
+    _check(_lib.simple_embed(ids.data_ptr(), table.data_ptr(), _stride(table), T, V, D, _TYPES[table.dtype], scale, out.data_ptr(), _stride(out),
+                             _current_stream()), "simple_embed")
+    return out
+
+
+def embed_grad(ids, dout, V: int, *, scale: float = 1.0, dtable=None, accumulate: bool = False):
+    """Gradient of ``embed`` for its table, [V, D] in dout's type, or in that of ``dtable`` (float32 or bfloat16) where it is given;
+    ``accumulate`` adds it to what ``dtable`` holds."""
+    _matrix(dout, "dout")
+    T, D = dout.shape
+    _tensor(ids, "ids", (T,), torch.int32, dout.device)
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate adds to dtable, and there is none")
+        dtable = torch.empty((V, D), dtype=dout.dtype, device=dout.device)
+    else:
+        _dtype(dtable, "dtable")
+        _tensor(dtable, "dtable", (V, D), dtable.dtype, dout.device)
+    ws = _workspace(_lib.simple_embed_grad_workspace(T, V, D), "simple_embed_grad_workspace", dout.device)
+    _check(_lib.simple_embed_grad(ids.data_ptr(), dout.data_ptr(), _stride(dout), T, V, D, _TYPES[dout.dtype], scale, dtable.data_ptr(),
+                                  _stride(dtable), _TYPES[dtable.dtype], int(accumulate), ws.data_ptr(), ws.numel(), _current_stream()),
+           "simple_embed_grad")
+    return dtable

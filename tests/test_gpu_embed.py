@@ -1,0 +1,106 @@
+"""Embedding lookup and its gradient against sums in 64 bits."""
+import pytest
+import torch
+
+from vocab_util import BF16, DEV, F32, F64, HALF, gen, laid, normal, padding_untouched, within
+
+pytestmark = pytest.mark.gpu
+
+
+def _ids(T, V, kind, g):
+    if kind == "one":
+        return torch.full((T,), V // 2, dtype=torch.int32, device=DEV)
+    if kind == "runs":   # a few ids, so that rows run over many chunks, ending at any place of them
+        return (torch.randint(0, 5, (T,), generator=g, device=DEV) * (V // 5)).to(torch.int32)
+    ids = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    if kind == "skewed":
+        ids = torch.where(torch.rand(T, generator=g, device=DEV) < 0.5, ids % 7, ids)
+    if kind == "invalid":
+        ids[::3] = -1
+        ids[1::5] = V
+        ids[2::7] = 2 ** 31 - 1
+    if kind == "nothing":
+        ids[:] = -1
+    return ids
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 8), (3, 1)])
+@pytest.mark.parametrize("T,V,D", [(1, 1, 1), (1, 1000, 4096), (33, 50, 7), (100, 333, 96), (257, 1024, 2056), (65, 500, 1001)])
+def test_lookup(T, V, D, pad, shift, dtype):
+    from paper_2512_00719_amd import vocab
+    g = gen(T + D)
+    table = laid(normal((V, D), dtype, g), pad, shift)
+    ids = _ids(T, V, "invalid" if T > 1 else "uniform", g)
+    out = laid(torch.zeros(T, D, dtype=dtype, device=DEV), pad, shift)
+    vocab.embed(ids, table, scale=1.7, out=out)
+    ok = (ids >= 0) & (ids < V)
+    want = torch.zeros(T, D, dtype=F32, device=DEV)
+    want[ok] = table[ids[ok].long()].float() * torch.tensor(1.7, dtype=F32, device=DEV)
+    assert torch.equal(out, want.to(dtype))
+    assert padding_untouched(out, pad, shift) if pad else True
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("kind", ["uniform", "skewed", "one", "runs", "invalid", "nothing"])
+@pytest.mark.parametrize("T,V,D", [(1, 1, 1), (31, 40, 7), (32, 600, 64), (33, 513, 65), (2047, 3000, 40), (2049, 511, 24), (4100, 262_143, 8), (9000, 512, 136),
+                                   (700, 50, 2064)])
+def test_gradient(T, V, D, kind, types):
+    """A token's term passes through its chunk's 32 additions and those of the chunks behind it: T / 32 + 32 roundings of 2^-24 on the sum of
+    the terms' magnitudes, then the scale's and, added to what was there, one more of float32 and that of the output's type."""
+    from paper_2512_00719_amd import vocab
+    g = gen(T * 7 + V)
+    ids = _ids(T, V, kind, g)
+    dout = normal((T, D), types[0], g)
+    ok = (ids >= 0) & (ids < V)
+    want, size = torch.zeros(V, D, dtype=F64, device=DEV), torch.zeros(V, D, dtype=F64, device=DEV)
+    want.index_add_(0, ids[ok].long(), dout[ok].to(F64))
+    size.index_add_(0, ids[ok].long(), dout[ok].to(F64).abs())
+    scale = float(torch.tensor(0.3, dtype=F32))
+    want, size = want * scale, size * scale
+    arith = (T / 32 + 32 + 3) * 2.0 ** -24
+    got = vocab.embed_grad(ids, dout, V, scale=0.3, dtable=torch.full((V, D), 5.0, dtype=types[1], device=DEV))
+    within(got, want, size * arith + want.abs() * HALF[types[1]], "gradient")
+    assert torch.equal(got, vocab.embed_grad(ids, dout, V, scale=0.3, dtable=torch.empty_like(got)))  # the same bits again
+    old = normal((V, D), types[1], g)
+    added = vocab.embed_grad(ids, dout, V, scale=0.3, dtable=old.clone(), accumulate=True)
+    total = want + old.to(F64)
+    within(added, total, size * arith + total.abs() * (HALF[types[1]] + 2.0 ** -24), "added gradient")
+    rest = torch.ones(V, dtype=torch.bool, device=DEV)
+    rest[ids[ok].long()] = False
+    assert torch.equal(added[rest], old[rest])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("pad,shift", [(1, 1), (8, 8), (8, 3)])
+def test_gradient_strides(pad, shift, dtype):
+    from paper_2512_00719_amd import vocab
+    g = gen(3)
+    ids = _ids(500, 90, "skewed", g)
+    dout = normal((500, 72), dtype, g)
+    want = vocab.embed_grad(ids, dout, 90)
+    for accumulate in (False, True):
+        got = laid(torch.zeros(90, 72, dtype=dtype, device=DEV), pad, shift)
+        vocab.embed_grad(ids, laid(dout, pad, shift), 90, dtable=got, accumulate=accumulate)
+        assert torch.equal(got, want) and padding_untouched(got, pad, shift)
+
+
+def test_no_tokens():
+    from paper_2512_00719_amd import vocab
+    table = torch.ones(10, 24, device=DEV)
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    assert vocab.embed(none, table).shape == (0, 24)
+    assert not vocab.embed_grad(none, table[:0], 10, dtable=table.clone()).any()
+    assert bool((vocab.embed_grad(none, table[:0], 10, dtable=table.clone(), accumulate=True) == 1).all())
+
+
+def test_gradient_is_that_of_the_lookup():
+    """L = sum(lookup * c) is linear in the table: its difference along d equals <gradient, d> but for roundings, 2^-24 a term."""
+    from paper_2512_00719_amd import vocab
+    g = gen(8)
+    ids = _ids(300, 40, "skewed", g)
+    table, d = normal((40, 33), F32, g), normal((40, 33), F32, g)
+    c = normal((300, 33), F32, g)
+    loss = lambda t: (vocab.embed(ids, t, scale=2.5).to(F64) * c.to(F64)).sum()  # noqa: E731
+    slope = float((vocab.embed_grad(ids, c, 40, scale=2.5).to(F64) * d.to(F64)).sum())
+    assert abs(float(loss(table + d) - loss(table - d)) / 2 - slope) < 2.0 ** -20 * float(2.5 * c.norm() * (table.norm() + d.norm())) * 300 ** 0.5
