@@ -1,0 +1,103 @@
+// The head in 8 bits: logits[t, v] = (sum over k of codes[t, k] * w_codes[v, k]) * scales[t] * w_scales[v], sums in 32-bit integers (exact), the
+// scales in float32, one rounding to the output's type.
+#include "simple_tiles.hpp"
+
+namespace simple {
+namespace head {
+
+using namespace tiles;
+
+constexpr int64_t MAX_K = 131071;  // 128 * 128 * K stays below 2^31
+
+struct Args {
+  Operand tokens, weights;
+  int k_bytes, np, nq, out_type;
+  bool vec;             // groups of four outputs may be stored together
+  const float *scales, *w_scales;
+  void* out;
+  int64_t out_stride;
+};
+
+template <typename T, bool VEC> __device__ __forceinline__ void put4(T* to, int64_t n, const float (&v)[4]) {
+  if (VEC && n >= 4) store<T, 4>(to, v);
+  else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) to[i] = down<T>(v[i]);
+  }
+}
+
+template <class S, bool DIRECT, typename T, bool VEC>
+__global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
+  int tp, tq;
+  tile_of(blockIdx.x, a.np, a.nq, tp, tq);
+  const int64_t p0 = (int64_t)tp * S::BP, q0 = (int64_t)tq * S::BQ;
+  typename S::Acc acc[S::FQ][S::FP];
+  product<S, DIRECT>(a.tokens, a.weights, p0, q0, a.k_bytes, lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t p1 = p0 + wave % S::NWP * S::FP * 16 + (lane & 15), q1 = q0 + wave / S::NWP * S::FQ * 16 + (lane >> 4) * 4;
+  const int64_t V = a.weights.rows;
+  float ws[S::FQ][4];
+#pragma unroll
+  for (int i = 0; i < S::FQ; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ws[i][e] = q1 + i * 16 + e < V ? a.w_scales[q1 + i * 16 + e] : 0.f;
+#pragma unroll
+  for (int j = 0; j < S::FP; ++j) {
+    const int64_t p = p1 + j * 16;
+    if (p >= a.tokens.rows) continue;
+    const float s = a.scales[p];
+    T* row = (T*)a.out + p * a.out_stride;
+#pragma unroll
+    for (int i = 0; i < S::FQ; ++i) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * s * ws[i][e];
+      put4<T, VEC>(row + q1 + i * 16, V - (q1 + i * 16), v);
+    }
+  }
+}
+
+template <class S, bool DIRECT> void launch(Args a, hipStream_t st) {
+  a.np = (int)ceil_div(a.tokens.rows, S::BP);
+  a.nq = (int)ceil_div(a.weights.rows, S::BQ);
+  const dim3 grid((unsigned)((int64_t)a.np * a.nq)), block(S::THREADS);
+  if (a.out_type == SIMPLE_F32) {
+    if (a.vec) hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float, false>), grid, block, 0, st, a);
+  } else {
+    if (a.vec) hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, uint16_t, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, uint16_t, false>), grid, block, 0, st, a);
+  }
+}
+template <bool DIRECT> void launch_for(const Args& a, hipStream_t st) {
+  const int64_t T = a.tokens.rows;
+  if (T <= 16) launch<Shape<Int8, 16, 64, 1, 4, 4>, DIRECT>(a, st);
+  else if (T <= 32) launch<Shape<Int8, 32, 64, 1, 4, 4>, DIRECT>(a, st);
+  else if (T <= 64) launch<Shape<Int8, 64, 64, 1, 4, 4>, DIRECT>(a, st);
+  else if (T <= 128) launch<Shape<Int8, 128, 128, 2, 2, 2>, DIRECT>(a, st);
+  else launch<Shape<Int8, 256, 256, 2, 4, 2>, DIRECT>(a, st);
+}
+
+}  // namespace head
+}  // namespace simple
+
+using namespace simple::head;
+
+extern "C" int simple_linear_int8(const int8_t* codes_dev, int64_t code_stride, const float* scales_dev, const int8_t* w_codes_dev,
+                                  int64_t w_code_stride, const float* w_scales_dev, int64_t T, int64_t V, int64_t K, void* out_dev,
+                                  int64_t out_stride, int out_dtype, void* hip_stream) {
+  if (T < 0 || V <= 0 || K <= 0 || code_stride < K || w_code_stride < K || out_stride < V || !good_type(out_dtype)) return SIMPLE_EINVAL;
+  if (K > MAX_K || T > ((int64_t)1 << 24) || V > ((int64_t)1 << 28)) return SIMPLE_ECAPACITY;
+  if (T == 0) return SIMPLE_OK;
+  if (!codes_dev || !scales_dev || !w_codes_dev || !w_scales_dev || !out_dev) return SIMPLE_EINVAL;
+  if (ceil_div(T, 16) * ceil_div(V, 64) > (int64_t)0x7FFFFFFF) return SIMPLE_ECAPACITY;
+  const int64_t e = type_bytes(out_dtype);
+  Args a{{(const unsigned char*)codes_dev, code_stride, T}, {(const unsigned char*)w_codes_dev, w_code_stride, V}, (int)K, 0, 0, out_dtype,
+         rows_aligned(out_dev, out_stride, e, 4 * e), scales_dev, w_scales_dev, out_dev, out_stride};
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (direct(a.tokens, K) && direct(a.weights, K)) launch_for<true>(a, st);
+  else launch_for<false>(a, st);
+  return launched();
+}

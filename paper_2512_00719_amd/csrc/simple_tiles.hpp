@@ -1,0 +1,215 @@
+// Matrix products out[p, q] = sum_k P[p, k] * Q[q, k] on the matrix cores: both operands row-major with k along the rows, of 16-bit
+// floating or 8-bit integer elements.  The kernels of the 8-bit head and of the cross entropy are made of this with
+// what they do to a finished tile.
+//
+// A workgroup forms a BP x BQ tile.  Rows are staged through LDS 128 bytes of k at a time; a fragment of 16 rows and 64 bytes
+// of k is one 16-byte read a lane whatever the element is, and feeds one 16x16 instruction (32 k of bfloat16, 64 of int8).
+// A row's 16-byte chunks are stored in the order chunk ^ (row & 7), so that the 16 rows of a fragment spread over all banks.
+#pragma once
+#include "simple_vocabdev.hpp"
+
+namespace simple {
+namespace tiles {
+
+using namespace vocab;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+struct Bf16 {
+  using Acc = f32x4;
+  static constexpr int BYTES = 2;
+  static __device__ __forceinline__ Acc mma(i32x4 a, i32x4 b, Acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+};
+struct Int8 {
+  using Acc = i32x4;
+  static constexpr int BYTES = 1;
+  static __device__ __forceinline__ Acc mma(i32x4 a, i32x4 b, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+};
+
+constexpr int KB = 128;  // bytes of k a step
+
+// One operand: `rows` rows of `k_bytes` bytes, `stride` bytes apart.
+struct Operand {
+  const unsigned char* p;
+  int64_t stride, rows;
+};
+
+// ---- staging by the memory system itself: 16 bytes a lane go from memory to LDS without a register ----
+// The wave's 64 lanes write 1 KB from `lds` on in lane order: 8 rows of a step.  Nothing here is seen by the compiler's own count of loads
+// in flight; arrived() below waits for them, and no register is written.
+__device__ __forceinline__ void to_lds(uint32_t lds, uint32_t offset, i32x4 resource, uint32_t k) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(resource), "s"(k) : "memory");
+}
+// All but the `N` newest of this wave's loads have arrived, and those of the workgroup's other waves; what the waves read of LDS before is in
+// their registers.
+template <int N> __device__ __forceinline__ void arrived() {
+  static_assert(N < 64, "six bits");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+// A buffer resource over the operand's rows from `row0` on, at most `n` of them.  Addresses behind its end read as zeros.
+__device__ __forceinline__ i32x4 resource_of(const Operand& o, int64_t row0, int n, int k_bytes) {
+  const int64_t left = o.rows - row0;
+  const uint32_t m = (uint32_t)(left < n ? left : n);
+  const uint64_t a = (uint64_t)(uintptr_t)(o.p + row0 * o.stride);
+  i32x4 r;
+  r.x = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+  r.y = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xFFFF);
+  r.z = __builtin_amdgcn_readfirstlane((int)((m - 1) * (uint32_t)o.stride + (uint32_t)k_bytes));
+  r.w = 0x00020000;
+  return r;
+}
+
+
+// A workgroup's tile, its waves (NWP along P times NWQ along Q), and how many steps are staged at once.
+template <class E_, int BP_, int BQ_, int NWP_, int NWQ_, int STAGES_> struct Shape {
+  using E = E_;
+  using Acc = typename E::Acc;
+  static constexpr int BP = BP_, BQ = BQ_, NWP = NWP_, NWQ = NWQ_, NW = NWP * NWQ, THREADS = 64 * NW, STAGES = STAGES_;
+  static constexpr int FP = BP / NWP / 16, FQ = BQ / NWQ / 16;                     // fragments a wave
+  static constexpr int GP = BP / 8, GQ = BQ / 8;                                   // groups of 8 rows, one load instruction each
+  static constexpr int LP = (GP + NW - 1) / NW, LQ = (GQ + NW - 1) / NW;           // loads a wave and step (more waves than groups: twice the same)
+  static constexpr int STAGE = (BP + BQ) * KB, LDS = STAGE * STAGES;
+  static_assert(FP * NWP * 16 == BP && FQ * NWQ * 16 == BQ && LDS <= 160 * 1024, "shape");
+};
+
+// Workgroup `id` of `np * nq` takes tile (p, q).  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets consecutive
+// places of an order in which GROUP tiles along P share their Q rows, so that what its 32 compute units read at a time is few rows of both.
+constexpr int XCDS = 8, GROUP = 8;
+__device__ __forceinline__ void tile_of(int id, int np, int nq, int& p, int& q) {
+  const int n = np * nq, per = n / XCDS, more = n % XCDS, x = id % XCDS;
+  const int at = x * per + min(x, more) + id / XCDS;
+  const int g = at / (GROUP * nq), first = g * GROUP, size = min(GROUP, np - first), r = at - first * nq;
+  p = first + r % size;
+  q = r / size;
+}
+
+// 16 bytes of a row from byte `k` on, zeros behind its end; any alignment.
+template <int BYTES> __device__ __forceinline__ i32x4 chunk_of(const unsigned char* row, int64_t k, int64_t k_bytes) {
+  i32x4 v = {0, 0, 0, 0};
+  if (k + 16 <= k_bytes) {
+    __builtin_memcpy(&v, row + k, 16);
+  } else if (k < k_bytes) {
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 16 / BYTES; ++i) {
+      const int at = i * BYTES;
+      if (k + at < k_bytes) {
+        const uint32_t e = BYTES == 1 ? (uint32_t)row[k + at] : (uint32_t)*reinterpret_cast<const uint16_t*>(row + k + at);
+        w[at / 4] |= e << (8 * (at % 4));
+      }
+    }
+    v = i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+  }
+  return v;
+}
+
+// acc[i][j] of a lane: rows q0 + (wave along Q * FQ + i) * 16 + (lane >> 4) * 4 + 0..3 of Q against row p0 + (wave along P * FP + j) * 16 + (lane & 15) of P.
+// Rows behind an operand's last repeat it (what they give is not stored).  DIRECT: rows are staged by to_lds(), which
+// wants them 16-byte aligned with k_bytes a multiple of 16; else through registers, any alignment.
+template <class S, bool DIRECT>
+__device__ __forceinline__ void product(const Operand& P, const Operand& Q, int64_t p0, int64_t q0, int k_bytes, unsigned char* lds,
+                                        typename S::Acc (&acc)[S::FQ][S::FP]) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wp = wave % S::NWP, wq = wave / S::NWP;
+  const int steps = (k_bytes + KB - 1) / KB;
+  const int row8 = lane >> 3, chunk = (lane & 7) ^ row8;  // what a lane stages of its group of 8 rows
+  const int p_rows = (int)min((int64_t)S::BP, P.rows - p0), q_rows = (int)min((int64_t)S::BQ, Q.rows - q0);
+#pragma unroll
+  for (int i = 0; i < S::FQ; ++i)
+#pragma unroll
+    for (int j = 0; j < S::FP; ++j) acc[i][j] = typename S::Acc{0, 0, 0, 0};
+  uint32_t at_p[2], at_q[2];  // the lane's place in the first fragment, for both halves of a step
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t c = (uint32_t)((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16;
+    at_p[h] = (wp * S::FP * 16 + (lane & 15)) * KB + c;
+    at_q[h] = S::BP * KB + (wq * S::FQ * 16 + (lane & 15)) * KB + c;
+  }
+  auto step = [&](int stage) {
+    const unsigned char* b = lds + stage * S::STAGE;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      i32x4 fp[S::FP], fq[S::FQ];
+#pragma unroll
+      for (int j = 0; j < S::FP; ++j) fp[j] = *reinterpret_cast<const i32x4*>(b + at_p[h] + j * 16 * KB);
+#pragma unroll
+      for (int i = 0; i < S::FQ; ++i) fq[i] = *reinterpret_cast<const i32x4*>(b + at_q[h] + i * 16 * KB);
+#pragma unroll
+      for (int i = 0; i < S::FQ; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FP; ++j) acc[i][j] = S::E::mma(fq[i], fp[j], acc[i][j]);
+    }
+  };
+  if constexpr (DIRECT) {
+    const i32x4 res_p = resource_of(P, p0, S::BP, k_bytes), res_q = resource_of(Q, q0, S::BQ, k_bytes);
+    uint32_t off_p[S::LP], off_q[S::LQ];
+#pragma unroll
+    for (int i = 0; i < S::LP; ++i) off_p[i] = (uint32_t)min((wave + i * S::NW) % S::GP * 8 + row8, p_rows - 1) * (uint32_t)P.stride + chunk * 16;
+#pragma unroll
+    for (int i = 0; i < S::LQ; ++i) off_q[i] = (uint32_t)min((wave + i * S::NW) % S::GQ * 8 + row8, q_rows - 1) * (uint32_t)Q.stride + chunk * 16;
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+    auto issue = [&](int s, int stage) {
+      const uint32_t b = base + stage * S::STAGE, k = (uint32_t)s * KB;
+      const bool behind = (int)k + chunk * 16 >= k_bytes;  // behind the row's end: an address behind the resource's, which reads as zeros
+#pragma unroll
+      for (int i = 0; i < S::LP; ++i) to_lds(b + (wave + i * S::NW) % S::GP * 1024, behind ? 0x80000000u : off_p[i], res_p, k);
+#pragma unroll
+      for (int i = 0; i < S::LQ; ++i) to_lds(b + S::BP * KB + (wave + i * S::NW) % S::GQ * 1024, behind ? 0x80000000u : off_q[i], res_q, k);
+    };
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s)
+      if (s < steps) issue(s, s);
+    int stage = 0;
+    for (int s = 0; s < steps; ++s) {
+      // the newest loads in flight are those of the steps behind this one
+      if (s + S::STAGES - 2 < steps) arrived<(S::STAGES - 2) * (S::LP + S::LQ)>();
+      else arrived<0>();
+      if (s + S::STAGES - 1 < steps) issue(s + S::STAGES - 1, stage == 0 ? S::STAGES - 1 : stage - 1);  // the stage of the step before: read by all
+      step(stage);
+      stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+    }
+    arrived<0>();  // (the caller may use the memory)
+  } else {
+    const unsigned char *row_p[S::LP], *row_q[S::LQ];
+#pragma unroll
+    for (int i = 0; i < S::LP; ++i) row_p[i] = P.p + (p0 + min((wave + i * S::NW) % S::GP * 8 + row8, p_rows - 1)) * P.stride;
+#pragma unroll
+    for (int i = 0; i < S::LQ; ++i) row_q[i] = Q.p + (q0 + min((wave + i * S::NW) % S::GQ * 8 + row8, q_rows - 1)) * Q.stride;
+    i32x4 v[S::LP + S::LQ];
+    auto fetch = [&](int s) {
+      const int64_t k = (int64_t)s * KB + chunk * 16;
+#pragma unroll
+      for (int i = 0; i < S::LP; ++i) v[i] = chunk_of<S::E::BYTES>(row_p[i], k, k_bytes);
+#pragma unroll
+      for (int i = 0; i < S::LQ; ++i) v[S::LP + i] = chunk_of<S::E::BYTES>(row_q[i], k, k_bytes);
+    };
+    auto put = [&](int stage) {
+      unsigned char* b = lds + stage * S::STAGE + lane * 16;
+#pragma unroll
+      for (int i = 0; i < S::LP; ++i) *reinterpret_cast<i32x4*>(b + (wave + i * S::NW) % S::GP * 1024) = v[i];
+#pragma unroll
+      for (int i = 0; i < S::LQ; ++i) *reinterpret_cast<i32x4*>(b + S::BP * KB + (wave + i * S::NW) % S::GQ * 1024) = v[S::LP + i];
+    };
+    fetch(0);
+    put(0);
+    for (int s = 0; s < steps; ++s) {
+      __syncthreads();
+      if (s + 1 < steps) fetch(s + 1);
+      step(s & 1);
+      if (s + 1 < steps) put((s + 1) & 1);  // read last in the step before, ahead of the barrier
+    }
+    __syncthreads();
+  }
+}
+
+// Whether product<S, true> takes the operand: its resource's offsets stay below 2^31.
+inline bool direct(const Operand& o, int64_t k_bytes) {
+  return ((uintptr_t)o.p & 15u) == 0 && (o.stride & 15) == 0 && (k_bytes & 15) == 0 && o.stride <= ((int64_t)1 << 22) && k_bytes <= ((int64_t)1 << 30);
+}
+
+}  // namespace tiles
+}  // namespace simple

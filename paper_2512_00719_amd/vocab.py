@@ -17,7 +17,7 @@ from . import binding
 from .binding import SIMPLE_BF16, SIMPLE_F32, SIMPLE_OK, SimpleError, _addresses, _current_stream
 
 EXPORTS = ("simple_rms_norm", "simple_rms_norm_int8", "simple_quantize_rows", "simple_rms_norm_grad", "simple_rms_norm_grad_workspace",
-           "simple_embed", "simple_embed_grad", "simple_embed_grad_workspace")
+           "simple_embed", "simple_embed_grad", "simple_embed_grad_workspace", "simple_linear_int8")
 
 
 def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
@@ -31,6 +31,7 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
         "simple_embed": (ci, vp, vp, i64, i64, i64, i64, ci, f32, vp, i64, vp),
         "simple_embed_grad": (ci, vp, vp, i64, i64, i64, i64, ci, f32, vp, i64, ci, ci, vp, i64, vp),
         "simple_embed_grad_workspace": (i64, i64, i64, i64),
+        "simple_linear_int8": (ci, vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, i64, ci, vp),
     }
     assert set(signatures) == set(EXPORTS)
     for name, (restype, *argtypes) in signatures.items():
@@ -196,3 +197,21 @@ def embed_grad(ids, dout, V: int, *, scale: float = 1.0, dtable=None, accumulate
                                   _stride(dtable), _TYPES[dtable.dtype], int(accumulate), ws.data_ptr(), ws.numel(), _current_stream()),
            "simple_embed_grad")
     return dtable
+
+
+def linear_int8(codes, scales, w_codes, w_scales, *, out_dtype: torch.dtype = torch.float32, out=None):
+    """Logits [T, V] of ``out_dtype`` (float32 or bfloat16): codes [T, K] times w_codes [V, K], both int8, times scales [T] and w_scales [V]."""
+    _matrix(codes, "codes", (torch.int8,))
+    T, K = codes.shape
+    V = w_codes.shape[0]
+    _tensor(scales, "scales", (T,), torch.float32, codes.device)
+    _tensor(w_codes, "w_codes", (V, K), torch.int8, codes.device)
+    _tensor(w_scales, "w_scales", (V,), torch.float32, codes.device)
+    if out is not None:
+        out_dtype = out.dtype
+    if out_dtype not in _TYPES:
+        raise TypeError(f"logits are float32 or bfloat16, got {out_dtype}")
+    out = _out(out, "out", (T, V), out_dtype, codes.device)
+    _check(_lib.simple_linear_int8(codes.data_ptr(), _stride(codes), scales.data_ptr(), w_codes.data_ptr(), _stride(w_codes), w_scales.data_ptr(),
+                                   T, V, K, out.data_ptr(), _stride(out), _TYPES[out_dtype], _current_stream()), "simple_linear_int8")
+    return out
