@@ -1,0 +1,460 @@
+// Softmax cross entropy of a head's logits z = c H W^T over a large vocabulary, without the [T, V] matrix, and its gradient.
+//
+// Forward: a workgroup forms a tile of logits in registers (simple_tiles.hpp), reduces it to a maximum and a sum of
+// exponentials a token, and passes these on; a second kernel joins the tiles' pairs:  M = max m, S = sum s exp(m - M), lse = M + log S.
+// The tile that holds a token's target also stores that logit.  Bound: the matrix rate, or for few tokens one read of the weights.
+//
+// Gradient: G = c dl (exp(z - lse) - [v = y]), dH = G W, dW = G^T H.  The vocabulary is taken in pieces; of a piece the logits are formed again (2 T V D more
+// operations; keeping them would take T V floats), turned into G in the registers, and G is kept for the two products, in both orders because the products want
+// k along the rows.  G is kept as bfloat16, each element rounded once from float32 (p - 1 is formed before): its error is of the
+// size of the outputs' own rounding.  dH is summed over the pieces in float32.
+// Tokens whose target is outside the vocabulary or whose dl is 0 take no part: their states are read as zeros where sums over tokens are
+// formed, so that a NaN in them stays with them.
+#include <algorithm>
+
+#include "simple_tiles.hpp"
+
+namespace simple {
+namespace xent {
+
+using namespace tiles;
+
+constexpr float LOG2E = 1.44269504088896340736f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+struct Pair { float m, s; };
+__device__ __forceinline__ Pair join(Pair a, Pair b) {
+  const float m = fmaxf(a.m, b.m), base = m == -INFINITY ? 0.f : m;  // (nothing in either: exp(-inf) twice)
+  return Pair{m, a.s * exp_of(a.m - base) + b.s * exp_of(b.m - base)};
+}
+
+struct Args {
+  Operand hidden, weight;  // of the weights: the piece's rows
+  int k_bytes, np, nq;
+  float scale;
+  const int32_t* targets;
+  int64_t V, v0;           // whole vocabulary, the piece's first row
+  // forward
+  Pair* pairs;             // [nq][T]
+  float* at_target;        // [T]
+  // gradient
+  const float *lse, *dloss;
+  uint16_t *g, *gt;        // [T][g_stride], [rows of the piece][gt_stride]; either may be null
+  int64_t g_stride, gt_stride;
+};
+
+template <class S, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void stats_kernel(Args a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
+  int tp, tq;
+  tile_of(blockIdx.x, a.np, a.nq, tp, tq);
+  const int64_t p0 = (int64_t)tp * S::BP, q0 = (int64_t)tq * S::BQ, T = a.hidden.rows;
+  typename S::Acc acc[S::FQ][S::FP];
+  product<S, DIRECT>(a.hidden, a.weight, p0, q0, a.k_bytes, lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
+  const int64_t q1 = q0 + wq * S::FQ * 16 + (lane >> 4) * 4;
+  const int left = (int)min((int64_t)S::BQ, a.V - q1);  // the lane's columns that exist
+  Pair(*part)[S::BP] = reinterpret_cast<Pair(*)[S::BP]>(lds);
+#pragma unroll
+  for (int j = 0; j < S::FP; ++j) {
+    const int pl = (wp * S::FP + j) * 16 + (lane & 15);
+    const int64_t p = p0 + pl;
+    const int64_t target = p < T ? (int64_t)a.targets[p] - q1 : -1;
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < S::FQ; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = i * 16 + e < left ? acc[i][j][e] * a.scale : -INFINITY;
+        acc[i][j][e] = z;
+        m = fmaxf(m, z);
+        if (target == i * 16 + e && i * 16 + e < left) a.at_target[p] = z;
+      }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float base = m == -INFINITY ? 0.f : m;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < S::FQ; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += exp_of(acc[i][j][e] - base);
+    s += __shfl_xor(s, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    if (lane < 16) part[wq][pl] = Pair{m, s};
+  }
+  __syncthreads();
+  for (int t = threadIdx.x; t < S::BP; t += S::THREADS) {
+    if (p0 + t >= T) break;
+    Pair v = part[0][t];
+#pragma unroll
+    for (int w = 1; w < S::NWQ; ++w) v = join(v, part[w][t]);
+    a.pairs[(int64_t)tq * T + p0 + t] = v;
+  }
+}
+
+// The tiles' pairs of 16 tokens a workgroup, by FIN_GROUPS groups of tiles.
+constexpr int FIN_T = 16, FIN_GROUPS = 64;
+__global__ __launch_bounds__(FIN_T * FIN_GROUPS) void finish_kernel(const Pair* pairs, int nq, int64_t T, int64_t V, const int32_t* targets,
+                                                                    const float* at_target, float* loss, float* lse) {
+  __shared__ Pair part[FIN_GROUPS][FIN_T];
+  const int lane = threadIdx.x % FIN_T, grp = threadIdx.x / FIN_T;
+  const int64_t t = (int64_t)blockIdx.x * FIN_T + lane;
+  Pair v{-INFINITY, 0.f};
+  if (t < T) {
+#pragma unroll 4
+    for (int q = grp; q < nq; q += FIN_GROUPS) v = join(v, pairs[(int64_t)q * T + t]);
+  }
+  part[grp][lane] = v;
+  for (int n = FIN_GROUPS / 2; n > 0; n /= 2) {
+    __syncthreads();
+    if (grp < n) part[grp][lane] = v = join(v, part[grp + n][lane]);
+  }
+  if (grp == 0 && t < T) {
+    const float l = v.m + logf(v.s);  // (a NaN logit is in s)
+    const int32_t y = targets[t];
+    lse[t] = l;
+    loss[t] = y >= 0 && y < V ? l - at_target[t] : 0.f;
+  }
+}
+
+__device__ __forceinline__ bool takes_part(int32_t target, float dloss, int64_t V) { return target >= 0 && target < V && dloss != 0.f; }
+
+// G of a tile, in both orders.  Columns behind the piece's last and tokens behind the last are zeros: sums run over them.
+template <class S, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void g_kernel(Args a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
+  int tp, tq;
+  tile_of(blockIdx.x, a.np, a.nq, tp, tq);
+  const int64_t p0 = (int64_t)tp * S::BP, q0 = (int64_t)tq * S::BQ, T = a.hidden.rows;
+  typename S::Acc acc[S::FQ][S::FP];
+  product<S, DIRECT>(a.hidden, a.weight, p0, q0, a.k_bytes, lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
+  const int64_t q1 = q0 + wq * S::FQ * 16 + (lane >> 4) * 4;
+  const int left = (int)min((int64_t)S::BQ, a.weight.rows - q1);
+#pragma unroll
+  for (int j = 0; j < S::FP; ++j) {
+    const int64_t p = p0 + (wp * S::FP + j) * 16 + (lane & 15);
+    const int32_t y = p < T ? a.targets[p] : -1;
+    const float dl = p < T ? a.dloss[p] : 0.f;
+    const bool on = takes_part(y, dl, a.V);
+    const float lse = on ? a.lse[p] : 0.f, d = dl * a.scale;
+    const int64_t target = (int64_t)y - a.v0 - q1;
+#pragma unroll
+    for (int i = 0; i < S::FQ; ++i) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float pr = exp_of(acc[i][j][e] * a.scale - lse);
+        v[e] = on && i * 16 + e < left ? (target == i * 16 + e ? pr - 1.f : pr) * d : 0.f;
+      }
+      if (a.g && p < T) store<uint16_t, 4>(a.g + p * a.g_stride + q1 + i * 16, v);
+      if (a.gt && p < a.gt_stride) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a.gt[(q1 + i * 16 + e) * a.gt_stride + p] = to_bf16(v[e]);
+      }
+    }
+  }
+}
+
+// out[c][r] = in[r][c] for bfloat16: rows behind the last and rows of tokens that take no part are zeros, up to `r_out` rows.
+constexpr int TT = 64;
+template <bool VEC>
+__global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* in, int64_t stride, int64_t rows, int64_t cols, uint16_t* out, int64_t out_stride,
+                                                        int64_t r_out, const int32_t* targets, const float* dloss, int64_t V) {
+  __shared__ uint16_t tile[TT][TT + 2];
+  const int64_t r0 = (int64_t)blockIdx.x * TT, c0 = (int64_t)blockIdx.y * TT;
+#pragma unroll
+  for (int u = 0; u < TT * TT / 8 / 256; ++u) {
+    const int i = u * 256 + threadIdx.x, r = i / (TT / 8), c = i % (TT / 8) * 8;
+    const int64_t rr = r0 + r, cc = c0 + c;
+    Group<uint16_t, 8> v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.v[e] = 0;
+    if (rr < rows && (!targets || takes_part(targets[rr], dloss[rr], V))) {
+      const uint16_t* p = in + rr * stride + cc;
+      if (VEC && cc + 8 <= cols) v = *reinterpret_cast<const Group<uint16_t, 8>*>(p);
+      else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (cc + e < cols) v.v[e] = p[e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) tile[r][c + e] = v.v[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < TT * TT / 8 / 256; ++u) {
+    const int i = u * 256 + threadIdx.x, c = i / (TT / 8), r = i % (TT / 8) * 8;
+    if (c0 + c >= cols || r0 + r >= r_out) continue;  // (r_out is a multiple of 8)
+    Group<uint16_t, 8> v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.v[e] = tile[r + e][c];
+    *reinterpret_cast<Group<uint16_t, 8>*>(out + (c0 + c) * out_stride + r0 + r) = v;
+  }
+}
+
+struct MulArgs {
+  Operand p, q;
+  int k_bytes, k_split, np, nq;  // each of gridDim.y workgroups of a tile takes k_split bytes of k
+  void* out;
+  int64_t stride, split_stride;
+  int type, add, vec;
+};
+// out[p][q] (+)= sum over k, in float32 or rounded once.
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
+  int tp, tq;
+  tile_of(blockIdx.x, a.np, a.nq, tp, tq);
+  const int64_t p0 = (int64_t)tp * S::BP, q0 = (int64_t)tq * S::BQ;
+  const int k0 = blockIdx.y * a.k_split;
+  a.p.p += k0;
+  a.q.p += k0;
+  typename S::Acc acc[S::FQ][S::FP];
+  product<S, true>(a.p, a.q, p0, q0, max(0, min(a.k_split, a.k_bytes - k0)), lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t p1 = p0 + wave % S::NWP * S::FP * 16 + (lane & 15), q1 = q0 + wave / S::NWP * S::FQ * 16 + (lane >> 4) * 4;
+  auto put = [&](auto* out) {
+    using T = std::remove_pointer_t<decltype(out)>;
+#pragma unroll
+    for (int j = 0; j < S::FP; ++j) {
+      if (p1 + j * 16 >= a.p.rows) continue;
+      T* row = out + blockIdx.y * a.split_stride + (p1 + j * 16) * a.stride;
+#pragma unroll
+      for (int i = 0; i < S::FQ; ++i) {
+        const int64_t q = q1 + i * 16;
+        float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        if (a.vec && q + 4 <= a.q.rows) {
+          if (a.add) {
+            float o[4];
+            load<T, 4>(row + q, o);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += o[e];
+          }
+          store<T, 4>(row + q, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (q + e < a.q.rows) row[q + e] = down<T>(a.add ? v[e] + up(row[q + e]) : v[e]);
+        }
+      }
+    }
+  };
+  if (a.type == SIMPLE_F32) put((float*)a.out);
+  else put((uint16_t*)a.out);
+}
+
+// dH: the splits' sums, in order; zeros for tokens that take no part.
+__global__ __launch_bounds__(256) void hidden_kernel(const float* sums, int splits, int64_t T, int64_t D, const int32_t* targets, const float* dloss,
+                                                     int64_t V, uint16_t* out, int64_t stride) {
+  const int64_t t = blockIdx.x;
+  const bool on = takes_part(targets[t], dloss[t], V);
+  for (int64_t c = threadIdx.x; c < D; c += 256) {
+    float v = 0.f;
+    if (on) {
+#pragma unroll 4
+      for (int s = 0; s < splits; ++s) v += sums[((int64_t)s * T + t) * D + c];
+    }
+    out[t * stride + c] = to_bf16(v);
+  }
+}
+
+// Tiles by the number of tokens: few tokens read every weight row once, in four stages that keep the memory busy; many run at the matrix rate.
+template <class E, typename F> void shaped(int64_t T, F&& f) {
+  if (T <= 16) f(Shape<E, 16, 64, 1, 4, 4>{});
+  else if (T <= 32) f(Shape<E, 32, 64, 1, 4, 4>{});
+  else if (T <= 64) f(Shape<E, 64, 64, 1, 4, 4>{});
+  else if (T <= 128) f(Shape<E, 128, 128, 2, 2, 2>{});
+  else f(Shape<E, 256, 256, 2, 4, 2>{});
+}
+int64_t tile_q(int64_t T) { return T <= 64 ? 64 : T <= 128 ? 128 : 256; }
+
+constexpr int64_t PIECE = (int64_t)1 << 27;   // values of G kept at a time (256 MB in each order)
+constexpr int64_t ROUND = 256;                // a piece's rows: a multiple of every tile
+constexpr int64_t MOST_ROWS = (int64_t)1 << 20;  // rows of G stay within what a buffer resource spans
+int64_t piece_rows(int64_t T, int64_t V) {
+  const int64_t most = std::min(MOST_ROWS, std::max<int64_t>(4096, PIECE / std::max<int64_t>(T, 1))), n = ceil_div(V, most);
+  return ceil_div(ceil_div(V, n), ROUND) * ROUND;
+}
+// Workgroups a tile of dH: enough to fill the chip, each with at least 16 steps of k.
+int hidden_splits(int64_t T, int64_t V, int64_t D) {
+  const int64_t bp = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : 256;
+  const int64_t tiles = std::max<int64_t>(1, ceil_div(T, bp) * ceil_div(D, tile_q(T))), want = T <= 64 ? 1024 : T <= 128 ? 512 : 256;
+  const int64_t most = std::max<int64_t>(1, piece_rows(T, V) * 2 / (16 * KB));
+  return (int)std::max<int64_t>(1, std::min(most, want / tiles));
+}
+
+struct Layout { int64_t g, gt, wt, ht, sums, total, rows, t16; int splits; };
+Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
+  Layout L{};
+  auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
+  L.rows = piece_rows(T, V);
+  L.t16 = ceil_div(T, 16) * 16;
+  if (hidden) {
+    L.splits = hidden_splits(T, V, D);
+    L.g = take(T * L.rows * 2);
+    L.wt = take(D * L.rows * 2);
+    L.sums = take((int64_t)L.splits * T * D * 4);
+  }
+  if (weight) {
+    L.gt = take(L.rows * L.t16 * 2);
+    L.ht = take(D * L.t16 * 2);
+  }
+  return L;
+}
+
+void transpose(const uint16_t* in, int64_t stride, int64_t rows, int64_t cols, uint16_t* out, int64_t out_stride, int64_t r_out, const int32_t* targets,
+               const float* dloss, int64_t V, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(r_out, TT), (unsigned)ceil_div(cols, TT));
+  if (rows_aligned(in, stride, 2, 16))
+    hipLaunchKernelGGL(transpose_kernel<true>, grid, dim3(256), 0, st, in, stride, rows, cols, out, out_stride, r_out, targets, dloss, V);
+  else
+    hipLaunchKernelGGL(transpose_kernel<false>, grid, dim3(256), 0, st, in, stride, rows, cols, out, out_stride, r_out, targets, dloss, V);
+}
+
+void multiply(MulArgs a, int splits, hipStream_t st) {
+  a.k_split = (int)(ceil_div(ceil_div(a.k_bytes, splits), KB) * KB);
+  a.vec = rows_aligned(a.out, a.stride, type_bytes(a.type), 4 * type_bytes(a.type));
+  shaped<Bf16>(a.p.rows, [&](auto shape) {
+    using S = decltype(shape);
+    a.np = (int)ceil_div(a.p.rows, S::BP);
+    a.nq = (int)ceil_div(a.q.rows, S::BQ);
+    hipLaunchKernelGGL(mul_kernel<S>, dim3((unsigned)(a.np * a.nq), (unsigned)splits), dim3(S::THREADS), 0, st, a);
+  });
+}
+
+}  // namespace xent
+}  // namespace simple
+
+using namespace simple::xent;
+
+namespace {
+constexpr int64_t MAX_T = (int64_t)1 << 20, MAX_V = (int64_t)1 << 28, MAX_D = 65536;
+
+int check_sizes(int64_t T, int64_t V, int64_t D) {
+  if (T < 0 || V <= 0 || D <= 0) return SIMPLE_EINVAL;
+  return T > MAX_T || V > MAX_V || D > MAX_D ? SIMPLE_ECAPACITY : SIMPLE_OK;
+}
+int64_t pairs_bytes(int64_t T, int64_t V) { return ((ceil_div(V, tile_q(T)) * T * (int64_t)sizeof(Pair) + 255) & ~(int64_t)255); }
+}  // namespace
+
+extern "C" int64_t simple_xent_workspace(int64_t T, int64_t V, int64_t D) {
+  const int rc = check_sizes(T, V, D);
+  return rc != SIMPLE_OK ? rc : pairs_bytes(T, V) + T * 4;
+}
+
+extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, const int32_t* targets_dev,
+                           int64_t T, int64_t V, int64_t D, float logit_scale, float* loss_dev, float* lse_dev, void* workspace_dev,
+                           int64_t workspace_bytes, void* hip_stream) {
+  const int rc = check_sizes(T, V, D);
+  if (rc != SIMPLE_OK) return rc;
+  if (hidden_stride < D || weight_stride < D) return SIMPLE_EINVAL;
+  if (T == 0) return SIMPLE_OK;
+  if (!hidden_dev || !weight_dev || !targets_dev || !loss_dev || !lse_dev) return SIMPLE_EINVAL;
+  if (!workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
+  if (workspace_bytes < simple_xent_workspace(T, V, D)) return SIMPLE_ECAPACITY;
+  hipStream_t st = (hipStream_t)hip_stream;
+  Args a{};
+  a.hidden = {(const unsigned char*)hidden_dev, hidden_stride * 2, T};
+  a.weight = {(const unsigned char*)weight_dev, weight_stride * 2, V};
+  a.k_bytes = (int)(D * 2);
+  a.scale = logit_scale;
+  a.targets = targets_dev;
+  a.V = V;
+  a.pairs = (Pair*)workspace_dev;
+  a.at_target = (float*)((unsigned char*)workspace_dev + pairs_bytes(T, V));
+  const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
+  shaped<Bf16>(T, [&](auto shape) {
+    using S = decltype(shape);
+    a.np = (int)ceil_div(T, S::BP);
+    a.nq = (int)ceil_div(V, S::BQ);
+    const dim3 grid((unsigned)((int64_t)a.np * a.nq)), block(S::THREADS);
+    if (dir) hipLaunchKernelGGL((stats_kernel<S, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((stats_kernel<S, false>), grid, block, 0, st, a);
+  });
+  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)ceil_div(T, FIN_T)), dim3(FIN_T * FIN_GROUPS), 0, st, (const Pair*)a.pairs, a.nq, T, V, targets_dev,
+                     (const float*)a.at_target, loss_dev, lse_dev);
+  return launched();
+}
+
+extern "C" int64_t simple_xent_grad_workspace(int64_t T, int64_t V, int64_t D, int want_dhidden, int want_dweight) {
+  const int rc = check_sizes(T, V, D);
+  return rc != SIMPLE_OK ? rc : layout(T, V, D, want_dhidden != 0, want_dweight != 0).total;
+}
+
+extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride,
+                                const int32_t* targets_dev, const float* lse_dev, int64_t T, int64_t V, int64_t D, float logit_scale,
+                                void* dhidden_dev, int64_t dhidden_stride, void* dweight_dev, int64_t dweight_stride, int dweight_dtype,
+                                int accumulate, void* workspace_dev, int64_t workspace_bytes, void* hip_stream) {
+  const int rc = check_sizes(T, V, D);
+  if (rc != SIMPLE_OK) return rc;
+  if (hidden_stride < D || weight_stride < D || (dhidden_dev && dhidden_stride < D) || (dweight_dev && dweight_stride < D)) return SIMPLE_EINVAL;
+  if (!good_type(dweight_dtype)) return SIMPLE_EINVAL;
+  if (T == 0) dhidden_dev = nullptr;
+  if (!dhidden_dev && (!dweight_dev || (T == 0 && accumulate))) return SIMPLE_OK;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const Layout L = layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr);
+  if (T > 0) {
+    if (!dloss_dev || !hidden_dev || !weight_dev || !targets_dev || !lse_dev || !workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
+    if (workspace_bytes < L.total) return SIMPLE_ECAPACITY;
+  }
+  unsigned char* ws = (unsigned char*)workspace_dev;
+  Args a{};
+  a.hidden = {(const unsigned char*)hidden_dev, hidden_stride * 2, T};
+  a.k_bytes = (int)(D * 2);
+  a.scale = logit_scale;
+  a.targets = targets_dev;
+  a.V = V;
+  a.lse = lse_dev;
+  a.dloss = dloss_dev;
+  if (dhidden_dev) { a.g = (uint16_t*)(ws + L.g); a.g_stride = L.rows; }
+  if (dweight_dev) { a.gt = (uint16_t*)(ws + L.gt); a.gt_stride = L.t16; }
+  const unsigned char* weight = (const unsigned char*)weight_dev;
+  if (dweight_dev && T > 0)
+    transpose((const uint16_t*)hidden_dev, hidden_stride, T, D, (uint16_t*)(ws + L.ht), L.t16, L.t16, targets_dev, dloss_dev, V, st);
+  for (int64_t v0 = 0; v0 < V; v0 += L.rows) {
+    const int64_t n = std::min(L.rows, V - v0), n8 = ceil_div(n, 8) * 8;
+    a.weight = {weight + v0 * weight_stride * 2, weight_stride * 2, n};
+    a.v0 = v0;
+    if (T > 0) {
+      const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
+      shaped<Bf16>(T, [&](auto shape) {
+        using S = decltype(shape);
+        a.np = (int)ceil_div(T, S::BP);
+        a.nq = (int)ceil_div(n, S::BQ);
+        const dim3 grid((unsigned)((int64_t)a.np * a.nq)), block(S::THREADS);
+        if (dir) hipLaunchKernelGGL((g_kernel<S, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((g_kernel<S, false>), grid, block, 0, st, a);
+      });
+    }
+    if (dhidden_dev) {
+      transpose((const uint16_t*)a.weight.p, weight_stride, n, D, (uint16_t*)(ws + L.wt), L.rows, n8, nullptr, nullptr, V, st);
+      MulArgs m{};
+      m.p = {(const unsigned char*)a.g, a.g_stride * 2, T};
+      m.q = {ws + L.wt, L.rows * 2, D};
+      m.k_bytes = (int)(n8 * 2);
+      m.out = ws + L.sums;
+      m.stride = D;
+      m.split_stride = T * D;
+      m.type = SIMPLE_F32;
+      m.add = v0 > 0;
+      multiply(m, L.splits, st);
+    }
+    if (dweight_dev) {
+      MulArgs m{};
+      m.p = {(const unsigned char*)a.gt, a.gt_stride * 2, n};
+      m.q = {ws + L.ht, L.t16 * 2, D};
+      m.k_bytes = (int)(L.t16 * 2);
+      m.out = (unsigned char*)dweight_dev + v0 * dweight_stride * type_bytes(dweight_dtype);
+      m.stride = dweight_stride;
+      m.type = dweight_dtype;
+      m.add = accumulate != 0;
+      multiply(m, 1, st);
+    }
+  }
+  if (dhidden_dev)
+    hipLaunchKernelGGL(hidden_kernel, dim3((unsigned)T), dim3(256), 0, st, (const float*)(ws + L.sums), L.splits, T, D, targets_dev, dloss_dev, V,
+                       (uint16_t*)dhidden_dev, dhidden_stride);
+  return launched();
+}

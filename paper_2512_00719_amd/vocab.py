@@ -17,7 +17,8 @@ from . import binding
 from .binding import SIMPLE_BF16, SIMPLE_F32, SIMPLE_OK, SimpleError, _addresses, _current_stream
 
 EXPORTS = ("simple_rms_norm", "simple_rms_norm_int8", "simple_quantize_rows", "simple_rms_norm_grad", "simple_rms_norm_grad_workspace",
-           "simple_embed", "simple_embed_grad", "simple_embed_grad_workspace", "simple_linear_int8")
+           "simple_embed", "simple_embed_grad", "simple_embed_grad_workspace", "simple_linear_int8",
+           "simple_xent", "simple_xent_workspace", "simple_xent_grad", "simple_xent_grad_workspace")
 
 
 def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
@@ -32,6 +33,10 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
         "simple_embed_grad": (ci, vp, vp, i64, i64, i64, i64, ci, f32, vp, i64, ci, ci, vp, i64, vp),
         "simple_embed_grad_workspace": (i64, i64, i64, i64),
         "simple_linear_int8": (ci, vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, i64, ci, vp),
+        "simple_xent": (ci, vp, i64, vp, i64, vp, i64, i64, i64, f32, vp, vp, vp, i64, vp),
+        "simple_xent_workspace": (i64, i64, i64, i64),
+        "simple_xent_grad": (ci, vp, vp, i64, vp, i64, vp, vp, i64, i64, i64, f32, vp, i64, vp, i64, ci, ci, vp, i64, vp),
+        "simple_xent_grad_workspace": (i64, i64, i64, i64, ci, ci),
     }
     assert set(signatures) == set(EXPORTS)
     for name, (restype, *argtypes) in signatures.items():
@@ -213,5 +218,52 @@ def linear_int8(codes, scales, w_codes, w_scales, *, out_dtype: torch.dtype = to
         raise TypeError(f"logits are float32 or bfloat16, got {out_dtype}")
     out = _out(out, "out", (T, V), out_dtype, codes.device)
     _check(_lib.simple_linear_int8(codes.data_ptr(), _stride(codes), scales.data_ptr(), w_codes.data_ptr(), _stride(w_codes), w_scales.data_ptr(),
-                                   T, V, K, out.data_ptr(), _stride(out), _TYPES[out_dtype], _current_stream()), "simple_linear_int8")
+                                   T, V, K, out.data_ptr(), _stride(out), _TYPES[out_dtype], _current_stream()), "simple_linear_int8",
+           "simple_xent", "simple_xent_workspace", "simple_xent_grad", "simple_xent_grad_workspace")
     return out
+
+
+def _xent_inputs(hidden, weight, targets):
+    _matrix(hidden, "hidden", (torch.bfloat16,))
+    T, D = hidden.shape
+    V = weight.shape[0]
+    _tensor(weight, "weight", (V, D), torch.bfloat16, hidden.device)
+    _tensor(targets, "targets", (T,), torch.int32, hidden.device)
+    return T, V, D
+
+
+def linear_xent(hidden, weight, targets, *, logit_scale: float = 1.0, loss=None, lse=None):
+    """``(loss, lse)``, float32 [T]: negative log-probability of ``targets`` (int32; outside the vocabulary: 0) under the logits
+    ``logit_scale * hidden @ weight.T``, and the logarithm of the sum of their exponentials.  bfloat16 operands."""
+    T, V, D = _xent_inputs(hidden, weight, targets)
+    loss = _out(loss, "loss", (T,), torch.float32, hidden.device)
+    lse = _out(lse, "lse", (T,), torch.float32, hidden.device)
+    ws = _workspace(_lib.simple_xent_workspace(T, V, D), "simple_xent_workspace", hidden.device)
+    _check(_lib.simple_xent(hidden.data_ptr(), _stride(hidden), weight.data_ptr(), _stride(weight), targets.data_ptr(), T, V, D, logit_scale,
+                            loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), _current_stream()), "simple_xent")
+    return loss, lse
+
+
+def linear_xent_grad(dloss, hidden, weight, targets, lse, *, logit_scale: float = 1.0, dhidden=None, dweight=None, accumulate: bool = False,
+                     need_dhidden: bool = True, need_dweight: bool = True):
+    """``(dhidden, dweight)``: gradients of ``(dloss * linear_xent(...)[0]).sum()``, in bfloat16 (``dweight`` in the type of the tensor given for it,
+    bfloat16 or float32, to which ``accumulate`` adds).  What is not needed is not formed and ``None``."""
+    T, V, D = _xent_inputs(hidden, weight, targets)
+    _tensor(dloss, "dloss", (T,), torch.float32, hidden.device)
+    _tensor(lse, "lse", (T,), torch.float32, hidden.device)
+    dhidden = _out(dhidden, "dhidden", (T, D), torch.bfloat16, hidden.device) if need_dhidden else None
+    if accumulate and need_dweight and dweight is None:
+        raise ValueError("accumulate adds to dweight, and there is none")
+    if not need_dweight:
+        dweight = None
+    elif dweight is None:
+        dweight = torch.empty((V, D), dtype=torch.bfloat16, device=hidden.device)
+    else:
+        _dtype(dweight, "dweight")
+        _tensor(dweight, "dweight", (V, D), dweight.dtype, hidden.device)
+    ws = _workspace(_lib.simple_xent_grad_workspace(T, V, D, int(need_dhidden), int(need_dweight)), "simple_xent_grad_workspace", hidden.device)
+    _check(_lib.simple_xent_grad(dloss.data_ptr(), hidden.data_ptr(), _stride(hidden), weight.data_ptr(), _stride(weight), targets.data_ptr(),
+                                 lse.data_ptr(), T, V, D, logit_scale, _ptr(dhidden), _stride(dhidden), _ptr(dweight), _stride(dweight),
+                                 SIMPLE_BF16 if dweight is None else _TYPES[dweight.dtype], int(accumulate), ws.data_ptr(), ws.numel(),
+                                 _current_stream()), "simple_xent_grad")
+    return dhidden, dweight
