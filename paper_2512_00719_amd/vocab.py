@@ -218,8 +218,7 @@ def linear_int8(codes, scales, w_codes, w_scales, *, out_dtype: torch.dtype = to
         raise TypeError(f"logits are float32 or bfloat16, got {out_dtype}")
     out = _out(out, "out", (T, V), out_dtype, codes.device)
     _check(_lib.simple_linear_int8(codes.data_ptr(), _stride(codes), scales.data_ptr(), w_codes.data_ptr(), _stride(w_codes), w_scales.data_ptr(),
-                                   T, V, K, out.data_ptr(), _stride(out), _TYPES[out_dtype], _current_stream()), "simple_linear_int8",
-           "simple_xent", "simple_xent_workspace", "simple_xent_grad", "simple_xent_grad_workspace")
+                                   T, V, K, out.data_ptr(), _stride(out), _TYPES[out_dtype], _current_stream()), "simple_linear_int8")
     return out
 
 
