@@ -6,8 +6,12 @@
 //
 // Gradient: G = c dl (exp(z - lse) - [v = y]), dH = G W, dW = G^T H.  The vocabulary is taken in pieces; of a piece the logits are formed again (2 T V D more
 // operations; keeping them would take T V floats), turned into G in the registers, and G is kept for the two products, in both orders because the products want
-// k along the rows.  G is kept as bfloat16, each element rounded once from float32 (p - 1 is formed before): its error is of the
-// size of the outputs' own rounding.  dH is summed over the pieces in float32.
+// k along the rows.  G is kept in 16 bits, and 16-bit floats of 11 bits it is: bfloat16's 8 cost the gradients twice the error of
+// their own rounding.  What their range lacks is made up for by powers of two, which round nothing: a token's row
+// (exp(z - lse) - [v = y]) has its largest magnitude, 1 - p_y, brought to 2^13 .. 2^14, so that a probability 2^-28 of it still has
+// its 11 bits (at 1 those of rare tokens, 1e-6 and below, would have had fewer than bfloat16's); the factor c dl goes with the token's states into the
+// product for dW, and behind the sum in dH; states and weights are brought below 2^14 by their largest magnitude.  Weights are then
+// exact (8 bits within 28 binades of the largest), G and the states rounded once, to 2^-12.  dH is summed over the pieces in float32.
 // Tokens whose target is outside the vocabulary or whose dl is 0 take no part: their states are read as zeros where sums over tokens are
 // formed, so that a NaN in them stays with them.
 #include <algorithm>
@@ -38,7 +42,7 @@ struct Args {
   Pair* pairs;             // [nq][T]
   float* at_target;        // [T]
   // gradient
-  const float *lse, *dloss;
+  const struct Token* tokens;
   uint16_t *g, *gt;        // [T][g_stride], [rows of the piece][gt_stride]; either may be null
   int64_t g_stride, gt_stride;
 };
@@ -117,7 +121,91 @@ __global__ __launch_bounds__(FIN_T * FIN_GROUPS) void finish_kernel(const Pair* 
   }
 }
 
-__device__ __forceinline__ bool takes_part(int32_t target, float dloss, int64_t V) { return target >= 0 && target < V && dloss != 0.f; }
+// What the gradient knows of a token: its target (-1: it takes no part), lse, the power of two on its row of G, and what the row still lacks of
+// the gradient, c dl over that power.
+struct Token { int32_t y; float lse, up, rest; };
+
+// Powers of two that bring values whose largest magnitude has the bits `top` below 2^14, and back.
+__device__ __forceinline__ float to_range(uint32_t top) {
+  const int e = (int)(top >> 23);  // (sign 0)
+  if (e == 0 || e == 255) return 1.f;
+  return __uint_as_float((uint32_t)min(max(267 - e, 14), 240) << 23);
+}
+__device__ __forceinline__ float from_range(uint32_t top) { return 1.f / to_range(top); }
+enum { TOP_STATES = 0, TOP_WEIGHTS = 1, TOPS = 2 };
+
+__global__ void clear_kernel(uint32_t* tops) { if (threadIdx.x < TOPS) tops[threadIdx.x] = 0u; }
+
+__device__ __forceinline__ void raise(uint32_t* top, float v) {  // the order of magnitudes' bits; the maximum does not depend on who comes first
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = __uint_as_float(max(__float_as_uint(v), (uint32_t)__shfl_xor((int)__float_as_uint(v), o, 64)));
+  if ((threadIdx.x & 63) == 0) atomicMax(top, __float_as_uint(v));
+}
+// The larger magnitude, a NaN above all.
+__device__ __forceinline__ float larger(float a, float b) { return __uint_as_float(max(__float_as_uint(a) & 0x7FFFFFFFu, __float_as_uint(b) & 0x7FFFFFFFu)); }
+
+struct PrepareArgs {
+  const uint16_t *hidden, *weight;
+  int64_t hidden_stride, weight_stride, T, V, D;
+  const int32_t* targets;
+  const float *lse, *dloss;
+  float scale;
+  Token* tokens;
+  uint32_t* tops;
+  int token_wgs;
+};
+// The first workgroups: a wave a token, its logit at the target once more (for the power of two alone, so its order of summation does not matter)
+// and its largest state.  The rest: the weights' largest magnitude, rows in turn.
+template <int VEC>
+__global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if ((int)blockIdx.x < a.token_wgs) {
+    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
+    if (t >= a.T) return;
+    const int32_t y = a.targets[t];
+    const float dl = a.dloss[t];
+    const bool on = y >= 0 && y < a.V && dl != 0.f;
+    Token k{-1, 0.f, 1.f, 0.f};
+    if (on) {
+      const uint16_t *h = a.hidden + t * a.hidden_stride, *w = a.weight + y * a.weight_stride;
+      float dot = 0.f, sizes = 0.f, top = 0.f;
+      for (int64_t c = lane * VEC; c < a.D; c += 64 * VEC) {
+        float x[VEC], v[VEC];
+        load<uint16_t, VEC>(h + c, x);
+        load<uint16_t, VEC>(w + c, v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) { dot = fmaf(x[e], v[e], dot); sizes = fmaf(fabsf(x[e]), fabsf(v[e]), sizes); top = larger(top, x[e]); }
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) { dot += __shfl_xor(dot, o, 64); sizes += __shfl_xor(sizes, o, 64); }
+      // 1 - p_y, and no less than what the logit may be off by here and in the tile (a random walk of D roundings): what is
+      // below that is noise, and must not be scaled beyond the type's range, 4 times the row's aim
+      const float lse = a.lse[t], left = -expm1f(dot * a.scale - lse);
+      const float noise = 5.9604645e-8f * (sqrtf((float)a.D) * sizes * fabsf(a.scale) + fabsf(lse) + 1.f);
+      const float most = left < noise ? noise : left;
+      const int e = (most < 1.f ? ilogbf(most) + 1 : 0) - 14;
+      k = Token{y, lse, ldexpf(1.f, -e), dl * a.scale * ldexpf(1.f, e)};
+      raise(a.tops + TOP_STATES, larger(top * k.rest, 0.f));
+    }
+    if (lane == 0) a.tokens[t] = k;
+    return;
+  }
+  float top = 0.f;
+  const int64_t waves = ((int64_t)gridDim.x - a.token_wgs) * 4;
+  for (int64_t v = ((int64_t)blockIdx.x - a.token_wgs) * 4 + wave; v < a.V; v += waves) {
+    const uint16_t* w = a.weight + v * a.weight_stride;
+#pragma unroll 8
+    for (int64_t c = lane * VEC; c < a.D; c += 64 * VEC) {
+      float x[VEC];
+      load<uint16_t, VEC>(w + c, x);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) top = larger(top, x[e]);
+    }
+  }
+  raise(a.tops + TOP_WEIGHTS, top);
+}
+
+__device__ __forceinline__ uint32_t f16_bits(float f) { return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)f); }
 
 // G of a tile, in both orders.  Columns behind the piece's last and tokens behind the last are zeros: sums run over them.
 template <class S, bool DIRECT>
@@ -129,58 +217,91 @@ __global__ __launch_bounds__(S::THREADS) void g_kernel(Args a) {
   typename S::Acc acc[S::FQ][S::FP];
   product<S, DIRECT>(a.hidden, a.weight, p0, q0, a.k_bytes, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
-  const int64_t q1 = q0 + wq * S::FQ * 16 + (lane >> 4) * 4;
+  const int ql = wq * S::FQ * 16 + (lane >> 4) * 4;  // the lane's first column in the tile
+  const int64_t q1 = q0 + ql;
   const int left = (int)min((int64_t)S::BQ, a.weight.rows - q1);
+  // A tile that LDS holds whole is turned there: two tokens of a column in a word, rows of 512 bytes whose 16-byte chunks are stored in an
+  // order that spreads a store's eight rows over the banks.  (Stored by single values, the second order took 25 of a tile's 130 us.)
+  constexpr bool TURN = S::BP * S::BQ * 2 <= S::LDS && S::BP == 256;
+  auto place = [](int q, int chunk) { return q * (S::BP * 2) + ((chunk ^ (((q >> 2) & 3) * 2 + (q & 1) * 8)) << 4); };
 #pragma unroll
   for (int j = 0; j < S::FP; ++j) {
-    const int64_t p = p0 + (wp * S::FP + j) * 16 + (lane & 15);
-    const int32_t y = p < T ? a.targets[p] : -1;
-    const float dl = p < T ? a.dloss[p] : 0.f;
-    const bool on = takes_part(y, dl, a.V);
-    const float lse = on ? a.lse[p] : 0.f, d = dl * a.scale;
-    const int64_t target = (int64_t)y - a.v0 - q1;
+    const int pl = (wp * S::FP + j) * 16 + (lane & 15);
+    const int64_t p = p0 + pl;
+    const Token k = p < T ? a.tokens[p] : Token{-1, 0.f, 1.f, 0.f};
+    const int64_t target = (int64_t)k.y - a.v0 - q1;
 #pragma unroll
     for (int i = 0; i < S::FQ; ++i) {
-      float v[4];
+      uint32_t v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float pr = exp_of(acc[i][j][e] * a.scale - lse);
-        v[e] = on && i * 16 + e < left ? (target == i * 16 + e ? pr - 1.f : pr) * d : 0.f;
+        const float pr = exp_of(acc[i][j][e] * a.scale - k.lse);
+        v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits((target == i * 16 + e ? pr - 1.f : pr) * k.up) : 0u;
       }
-      if (a.g && p < T) store<uint16_t, 4>(a.g + p * a.g_stride + q1 + i * 16, v);
-      if (a.gt && p < a.gt_stride) {
+      if (a.g && p < T) *reinterpret_cast<uint2*>(a.g + p * a.g_stride + q1 + i * 16) = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
+      if constexpr (TURN) {
+        if (a.gt) {
+          // of each pair of columns the even lane takes the first for both tokens, the odd one the second
+          const bool odd = lane & 1;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) a.gt[(q1 + i * 16 + e) * a.gt_stride + p] = to_bf16(v[e]);
+          for (int e = 0; e < 4; e += 2) {
+            const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? v[e] : v[e + 1]), 0xB1, 0xF, 0xF, true);  // quad_perm 1 0 3 2
+            const int q = ql + i * 16 + e + odd;
+            *reinterpret_cast<uint32_t*>(lds + place(q, pl >> 3) + (pl & 6) * 2) = odd ? other | v[e + 1] << 16 : v[e] | other << 16;
+          }
+        }
+      } else if (a.gt && p < a.gt_stride) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a.gt[(q1 + i * 16 + e) * a.gt_stride + p] = (uint16_t)v[e];
       }
+    }
+  }
+  if constexpr (TURN) {
+    if (!a.gt) return;
+    __syncthreads();
+    constexpr int CHUNKS = S::BP / 8;  // of a row
+    for (int n = threadIdx.x; n < S::BQ * CHUNKS; n += S::THREADS) {
+      const int q = n / CHUNKS, c = n % CHUNKS;
+      if (p0 + c * 8 < a.gt_stride)  // (a multiple of 16)
+        *reinterpret_cast<i32x4*>(a.gt + (q0 + q) * a.gt_stride + p0 + c * 8) = *reinterpret_cast<const i32x4*>(lds + place(q, c));
     }
   }
 }
 
-// out[c][r] = in[r][c] for bfloat16: rows behind the last and rows of tokens that take no part are zeros, up to `r_out` rows.
+// out[c][r] = in[r][c], from bfloat16 to 16-bit floats of 11 bits in range: rows behind the last and rows of tokens that take no part are zeros,
+// up to `r_out` rows.
 constexpr int TT = 64;
 template <bool VEC>
 __global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* in, int64_t stride, int64_t rows, int64_t cols, uint16_t* out, int64_t out_stride,
-                                                        int64_t r_out, const int32_t* targets, const float* dloss, int64_t V) {
+                                                        int64_t r_out, const Token* tokens, const uint32_t* top) {
   __shared__ uint16_t tile[TT][TT + 2];
   const int64_t r0 = (int64_t)blockIdx.x * TT, c0 = (int64_t)blockIdx.y * TT;
+  const float range = to_range(*top);
 #pragma unroll
   for (int u = 0; u < TT * TT / 8 / 256; ++u) {
     const int i = u * 256 + threadIdx.x, r = i / (TT / 8), c = i % (TT / 8) * 8;
     const int64_t rr = r0 + r, cc = c0 + c;
-    Group<uint16_t, 8> v;
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v.v[e] = 0;
-    if (rr < rows && (!targets || takes_part(targets[rr], dloss[rr], V))) {
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    float m = range;
+    bool on = rr < rows;
+    if (on && tokens) {
+      const Token k = tokens[rr];
+      on = k.y >= 0;
+      m *= k.rest;
+    }
+    if (on) {
       const uint16_t* p = in + rr * stride + cc;
-      if (VEC && cc + 8 <= cols) v = *reinterpret_cast<const Group<uint16_t, 8>*>(p);
+      if (VEC && cc + 8 <= cols) load<uint16_t, 8>(p, v);
       else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (cc + e < cols) v.v[e] = p[e];
+          if (cc + e < cols) v[e] = up(p[e]);
       }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) tile[r][c + e] = v.v[e];
+    for (int e = 0; e < 8; ++e) tile[r][c + e] = (uint16_t)f16_bits(v[e] * m);
   }
   __syncthreads();
 #pragma unroll
@@ -200,6 +321,7 @@ struct MulArgs {
   void* out;
   int64_t stride, split_stride;
   int type, add, vec;
+  const uint32_t* top;           // not null: the sums are brought back by from_range
 };
 // out[p][q] (+)= sum over k, in float32 or rounded once.
 template <class S>
@@ -215,6 +337,7 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
   product<S, true>(a.p, a.q, p0, q0, max(0, min(a.k_split, a.k_bytes - k0)), lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t p1 = p0 + wave % S::NWP * S::FP * 16 + (lane & 15), q1 = q0 + wave / S::NWP * S::FQ * 16 + (lane >> 4) * 4;
+  const float back = a.top ? from_range(*a.top) : 1.f;
   auto put = [&](auto* out) {
     using T = std::remove_pointer_t<decltype(out)>;
 #pragma unroll
@@ -224,7 +347,7 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
 #pragma unroll
       for (int i = 0; i < S::FQ; ++i) {
         const int64_t q = q1 + i * 16;
-        float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        float v[4] = {acc[i][j][0] * back, acc[i][j][1] * back, acc[i][j][2] * back, acc[i][j][3] * back};
         if (a.vec && q + 4 <= a.q.rows) {
           if (a.add) {
             float o[4];
@@ -245,18 +368,19 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
   else put((uint16_t*)a.out);
 }
 
-// dH: the splits' sums, in order; zeros for tokens that take no part.
-__global__ __launch_bounds__(256) void hidden_kernel(const float* sums, int splits, int64_t T, int64_t D, const int32_t* targets, const float* dloss,
-                                                     int64_t V, uint16_t* out, int64_t stride) {
+// dH: the splits' sums, in order, times what G's rows and the weights' range lack; zeros for tokens that take no part.
+__global__ __launch_bounds__(256) void hidden_kernel(const float* sums, int splits, int64_t T, int64_t D, const Token* tokens, const uint32_t* top,
+                                                     uint16_t* out, int64_t stride) {
   const int64_t t = blockIdx.x;
-  const bool on = takes_part(targets[t], dloss[t], V);
+  const Token k = tokens[t];
+  const float m = k.rest * from_range(*top);
   for (int64_t c = threadIdx.x; c < D; c += 256) {
     float v = 0.f;
-    if (on) {
+    if (k.y >= 0) {
 #pragma unroll 4
       for (int s = 0; s < splits; ++s) v += sums[((int64_t)s * T + t) * D + c];
     }
-    out[t * stride + c] = to_bf16(v);
+    out[t * stride + c] = to_bf16(k.y >= 0 ? v * m : 0.f);
   }
 }
 
@@ -285,12 +409,14 @@ int hidden_splits(int64_t T, int64_t V, int64_t D) {
   return (int)std::max<int64_t>(1, std::min(most, want / tiles));
 }
 
-struct Layout { int64_t g, gt, wt, ht, sums, total, rows, t16; int splits; };
+struct Layout { int64_t tops, tokens, g, gt, wt, ht, sums, total, rows, t16; int splits; };
 Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
   Layout L{};
   auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
   L.rows = piece_rows(T, V);
   L.t16 = ceil_div(T, 16) * 16;
+  L.tops = take(TOPS * 4);
+  L.tokens = take(T * (int64_t)sizeof(Token));
   if (hidden) {
     L.splits = hidden_splits(T, V, D);
     L.g = take(T * L.rows * 2);
@@ -304,19 +430,19 @@ Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
   return L;
 }
 
-void transpose(const uint16_t* in, int64_t stride, int64_t rows, int64_t cols, uint16_t* out, int64_t out_stride, int64_t r_out, const int32_t* targets,
-               const float* dloss, int64_t V, hipStream_t st) {
+void transpose(const uint16_t* in, int64_t stride, int64_t rows, int64_t cols, uint16_t* out, int64_t out_stride, int64_t r_out, const Token* tokens,
+               const uint32_t* top, hipStream_t st) {
   const dim3 grid((unsigned)ceil_div(r_out, TT), (unsigned)ceil_div(cols, TT));
   if (rows_aligned(in, stride, 2, 16))
-    hipLaunchKernelGGL(transpose_kernel<true>, grid, dim3(256), 0, st, in, stride, rows, cols, out, out_stride, r_out, targets, dloss, V);
+    hipLaunchKernelGGL(transpose_kernel<true>, grid, dim3(256), 0, st, in, stride, rows, cols, out, out_stride, r_out, tokens, top);
   else
-    hipLaunchKernelGGL(transpose_kernel<false>, grid, dim3(256), 0, st, in, stride, rows, cols, out, out_stride, r_out, targets, dloss, V);
+    hipLaunchKernelGGL(transpose_kernel<false>, grid, dim3(256), 0, st, in, stride, rows, cols, out, out_stride, r_out, tokens, top);
 }
 
 void multiply(MulArgs a, int splits, hipStream_t st) {
   a.k_split = (int)(ceil_div(ceil_div(a.k_bytes, splits), KB) * KB);
   a.vec = rows_aligned(a.out, a.stride, type_bytes(a.type), 4 * type_bytes(a.type));
-  shaped<Bf16>(a.p.rows, [&](auto shape) {
+  shaped<F16>(a.p.rows, [&](auto shape) {
     using S = decltype(shape);
     a.np = (int)ceil_div(a.p.rows, S::BP);
     a.nq = (int)ceil_div(a.q.rows, S::BQ);
@@ -406,13 +532,25 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   a.scale = logit_scale;
   a.targets = targets_dev;
   a.V = V;
-  a.lse = lse_dev;
-  a.dloss = dloss_dev;
+  uint32_t* tops = (uint32_t*)(ws + L.tops);
+  Token* tokens = (Token*)(ws + L.tokens);
+  a.tokens = tokens;
   if (dhidden_dev) { a.g = (uint16_t*)(ws + L.g); a.g_stride = L.rows; }
   if (dweight_dev) { a.gt = (uint16_t*)(ws + L.gt); a.gt_stride = L.t16; }
   const unsigned char* weight = (const unsigned char*)weight_dev;
-  if (dweight_dev && T > 0)
-    transpose((const uint16_t*)hidden_dev, hidden_stride, T, D, (uint16_t*)(ws + L.ht), L.t16, L.t16, targets_dev, dloss_dev, V, st);
+  if (T > 0) {
+    hipLaunchKernelGGL(clear_kernel, dim3(1), dim3(64), 0, st, tops);
+    PrepareArgs r{(const uint16_t*)hidden_dev, (const uint16_t*)weight_dev, hidden_stride, weight_stride, T, V, D, targets_dev, lse_dev, dloss_dev,
+                  logit_scale, tokens, tops, (int)ceil_div(T, 4)};
+    // (the weights' range is dH's: its product alone reads them in 16-bit floats)
+    const dim3 grid((unsigned)(r.token_wgs + (dhidden_dev ? std::min<int64_t>(2048, ceil_div(V, 4)) : 0)));
+    if (D % 8 == 0 && rows_aligned(hidden_dev, hidden_stride, 2, 16) && rows_aligned(weight_dev, weight_stride, 2, 16))
+      hipLaunchKernelGGL(prepare_kernel<8>, grid, dim3(256), 0, st, r);
+    else
+      hipLaunchKernelGGL(prepare_kernel<1>, grid, dim3(256), 0, st, r);
+    if (dweight_dev)
+      transpose((const uint16_t*)hidden_dev, hidden_stride, T, D, (uint16_t*)(ws + L.ht), L.t16, L.t16, tokens, tops + TOP_STATES, st);
+  }
   for (int64_t v0 = 0; v0 < V; v0 += L.rows) {
     const int64_t n = std::min(L.rows, V - v0), n8 = ceil_div(n, 8) * 8;
     a.weight = {weight + v0 * weight_stride * 2, weight_stride * 2, n};
@@ -429,7 +567,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       });
     }
     if (dhidden_dev) {
-      transpose((const uint16_t*)a.weight.p, weight_stride, n, D, (uint16_t*)(ws + L.wt), L.rows, n8, nullptr, nullptr, V, st);
+      transpose((const uint16_t*)a.weight.p, weight_stride, n, D, (uint16_t*)(ws + L.wt), L.rows, n8, nullptr, tops + TOP_WEIGHTS, st);
       MulArgs m{};
       m.p = {(const unsigned char*)a.g, a.g_stride * 2, T};
       m.q = {ws + L.wt, L.rows * 2, D};
@@ -450,11 +588,12 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       m.stride = dweight_stride;
       m.type = dweight_dtype;
       m.add = accumulate != 0;
+      m.top = T > 0 ? tops + TOP_STATES : nullptr;
       multiply(m, 1, st);
     }
   }
   if (dhidden_dev)
-    hipLaunchKernelGGL(hidden_kernel, dim3((unsigned)T), dim3(256), 0, st, (const float*)(ws + L.sums), L.splits, T, D, targets_dev, dloss_dev, V,
-                       (uint16_t*)dhidden_dev, dhidden_stride);
+    hipLaunchKernelGGL(hidden_kernel, dim3((unsigned)T), dim3(256), 0, st, (const float*)(ws + L.sums), L.splits, T, D, tokens,
+                       tops + TOP_WEIGHTS, (uint16_t*)dhidden_dev, dhidden_stride);
   return launched();
 }
