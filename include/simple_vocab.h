@@ -92,8 +92,8 @@ int simple_linear_int8(const int8_t* codes_dev, int64_t code_stride, const float
  * Cross entropy of logits z = logit_scale * hidden * weight^T (hidden [T, D], weight [V, D], both bfloat16; sums float32), of which no [T, V]
  * matrix is kept:
  *   lse[t] = log(sum over v of exp z[t, v]),   loss[t] = lse[t] - z[t, targets[t]]
- * loss is the negative log-probability of the target, 0 where the target is outside [0, V) (a token that is masked).  logit_scale is 1 / temperature
- * for tokens that were drawn at one.  workspace_dev: simple_xent_workspace(T, V, D) bytes, 16-byte aligned.  T <= 2^20, V <= 2^28, D <= 65536.
+ * loss is the negative log-probability of the target, 0 where the target is outside [0, V) (a token that is masked).  logit_scale (positive) is
+ * 1 / temperature for tokens that were drawn at one.  workspace_dev: simple_xent_workspace(T, V, D) bytes, 16-byte aligned.  T <= 2^20, V <= 2^28, D <= 65536.
  */
 int simple_xent(const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, const int32_t* targets_dev,
                 int64_t T, int64_t V, int64_t D, float logit_scale, float* loss_dev, float* lse_dev, void* workspace_dev,

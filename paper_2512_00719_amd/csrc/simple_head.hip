@@ -11,7 +11,8 @@ constexpr int64_t MAX_K = 131071;  // 128 * 128 * K stays below 2^31
 
 struct Args {
   Operand tokens, weights;
-  int k_bytes, np, nq, out_type;
+  int k_bytes, out_type;
+  Plan plan;
   bool vec;             // groups of four outputs may be stored together
   const float *scales, *w_scales;
   void* out;
@@ -28,11 +29,7 @@ template <typename T, bool VEC> __device__ __forceinline__ void put4(T* to, int6
 }
 
 template <class S, bool DIRECT, typename T, bool VEC>
-__global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
-  __shared__ __align__(1024) unsigned char lds[S::LDS];
-  int tp, tq;
-  tile_of(blockIdx.x, a.np, a.nq, tp, tq);
-  const int64_t p0 = (int64_t)tp * S::BP, q0 = (int64_t)tq * S::BQ;
+__device__ __forceinline__ void linear_int8_tile(const Args& a, int64_t p0, int64_t q0, unsigned char* lds) {
   typename S::Acc acc[S::FQ][S::FP];
   product<S, DIRECT>(a.tokens, a.weights, p0, q0, a.k_bytes, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -58,11 +55,15 @@ __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
     }
   }
 }
+template <class S, bool DIRECT, typename T, bool VEC>
+__global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
+  tile_of<S>(a.plan, a.tokens.rows, [&](auto shape, int64_t p0, int64_t q0) { linear_int8_tile<decltype(shape), DIRECT, T, VEC>(a, p0, q0, lds); });
+}
 
 template <class S, bool DIRECT> void launch(Args a, hipStream_t st) {
-  a.np = (int)ceil_div(a.tokens.rows, S::BP);
-  a.nq = (int)ceil_div(a.weights.rows, S::BQ);
-  const dim3 grid((unsigned)((int64_t)a.np * a.nq)), block(S::THREADS);
+  a.plan = plan<S>(a.tokens.rows, a.weights.rows);
+  const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
   if (a.out_type == SIMPLE_F32) {
     if (a.vec) hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float, false>), grid, block, 0, st, a);
@@ -94,7 +95,7 @@ extern "C" int simple_linear_int8(const int8_t* codes_dev, int64_t code_stride, 
   if (!codes_dev || !scales_dev || !w_codes_dev || !w_scales_dev || !out_dev) return SIMPLE_EINVAL;
   if (ceil_div(T, 16) * ceil_div(V, 64) > (int64_t)0x7FFFFFFF) return SIMPLE_ECAPACITY;
   const int64_t e = type_bytes(out_dtype);
-  Args a{{(const unsigned char*)codes_dev, code_stride, T}, {(const unsigned char*)w_codes_dev, w_code_stride, V}, (int)K, 0, 0, out_dtype,
+  Args a{{(const unsigned char*)codes_dev, code_stride, T}, {(const unsigned char*)w_codes_dev, w_code_stride, V}, (int)K, out_dtype, Plan{},
          rows_aligned(out_dev, out_stride, e, 4 * e), scales_dev, w_scales_dev, out_dev, out_stride};
   hipStream_t st = (hipStream_t)hip_stream;
   if (direct(a.tokens, K) && direct(a.weights, K)) launch_for<true>(a, st);

@@ -84,15 +84,48 @@ template <class E_, int BP_, int BQ_, int NWP_, int NWQ_, int STAGES_> struct Sh
   static_assert(FP * NWP * 16 == BP && FQ * NWQ * 16 == BQ && LDS <= 160 * 1024, "shape");
 };
 
-// Workgroup `id` of `np * nq` takes tile (p, q).  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets consecutive
-// places of an order in which GROUP tiles along P share their Q rows, so that what its 32 compute units read at a time is few rows of both.
-constexpr int XCDS = 8, GROUP = 8;
-__device__ __forceinline__ void tile_of(int id, int np, int nq, int& p, int& q) {
-  const int n = np * nq, per = n / XCDS, more = n % XCDS, x = id % XCDS;
-  const int at = x * per + min(x, more) + id / XCDS;
+// The order of `np * nq` tiles.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets consecutive places of an order in
+// which GROUP tiles along P share their Q rows, so that what its 32 compute units read at a time is few rows of both.
+constexpr int XCDS = 8, GROUP = 8, CUS = 256;
+__device__ __forceinline__ void tile_at(int at, int np, int nq, int& p, int& q) {
   const int g = at / (GROUP * nq), first = g * GROUP, size = min(GROUP, np - first), r = at - first * nq;
   p = first + r % size;
   q = r / size;
+}
+__device__ __forceinline__ int place_of(int id, int n) {
+  const int per = n / XCDS, more = n % XCDS, x = id % XCDS;
+  return x * per + min(x, more) + id / XCDS;
+}
+
+// A tile that fills a compute unit takes it alone, so that tiles run in rounds of CUS.  Tiles of a last round that is at most a quarter full are cut in
+// four along P instead, eight waves to each part, a compute unit to each: the round then takes about 0.35 of a whole one.
+template <class S> struct Cut {
+  static constexpr bool CAN = S::BP == 256 && S::BQ == 256;
+  using Part = Shape<typename S::E, CAN ? 64 : S::BP, S::BQ, CAN ? 1 : S::NWP, CAN ? 8 : S::NWQ, S::STAGES>;
+};
+struct Plan { int np, nq, whole, grid; };  // whole tiles, and workgroups in all
+template <class S> inline Plan plan(int64_t p_rows, int64_t q_rows, bool may_cut = true) {
+  Plan r{(int)ceil_div(p_rows, S::BP), (int)ceil_div(q_rows, S::BQ), 0, 0};
+  const int n = r.np * r.nq, last = n % CUS;
+  const bool cut = may_cut && Cut<S>::CAN && last > 0 && last * 4 <= CUS;
+  r.whole = cut ? n - last : n;
+  r.grid = r.whole + (n - r.whole) * 4;
+  return r;
+}
+// Calls f(shape, p0, q0) for the workgroup's tile or part of one.
+template <class S, typename F> __device__ __forceinline__ void tile_of(const Plan& r, int64_t p_rows, F&& f) {
+  int p, q;
+  if constexpr (Cut<S>::CAN) {
+    if ((int)blockIdx.x >= r.whole) {
+      const int i = place_of((int)blockIdx.x - r.whole, r.grid - r.whole);
+      tile_at(r.whole + i / 4, r.np, r.nq, p, q);
+      const int64_t p0 = (int64_t)p * S::BP + i % 4 * Cut<S>::Part::BP;
+      if (p0 < p_rows) f(typename Cut<S>::Part{}, p0, (int64_t)q * S::BQ);
+      return;
+    }
+  }
+  tile_at(place_of((int)blockIdx.x, r.whole), r.np, r.nq, p, q);
+  f(S{}, (int64_t)p * S::BP, (int64_t)q * S::BQ);
 }
 
 // 16 bytes of a row from byte `k` on, zeros behind its end; any alignment.
@@ -180,7 +213,7 @@ __device__ __forceinline__ void product(const Operand& P, const Operand& Q, int6
       // one at a time between groups of products: eight in a row fill the memory pipeline's queue, and the wave waits there with its products (bfloat16
       // 8192 x 128,256 x 4096: 1.34 PFLOP/s so, 1.26 with the loads in front, 1.24 with neither).
       constexpr int NF = S::FP + S::FQ, NL = S::LP + S::LQ, NM = S::FP * S::FQ, GROUPS = 8, MG = NM / GROUPS, RG = GROUPS - 2;
-      static_assert(NM % GROUPS == 0 && NL <= GROUPS, "groups");
+      static_assert(NM % GROUPS == 0, "groups");
       i32x4 fp0[S::FP], fq0[S::FQ], fp1[S::FP], fq1[S::FQ];
       auto half = [&](i32x4 (&fp)[S::FP], i32x4 (&fq)[S::FQ], bool next, int stage, int h, i32x4 (&np)[S::FP], i32x4 (&nq)[S::FQ], bool more, int s, int to) {
 #pragma unroll
@@ -189,7 +222,10 @@ __device__ __forceinline__ void product(const Operand& P, const Operand& Q, int6
 #pragma unroll
             for (int n = g * NF / RG; n < min(NF, (g + 1) * NF / RG); ++n) read(stage, h, n, np, nq);
           }
-          if (more && g < NL) load(s, to, g);
+          if (more) {
+#pragma unroll
+            for (int n = g * NL / GROUPS; n < (g + 1) * NL / GROUPS; ++n) load(s, to, n);
+          }
 #pragma unroll
           for (int m = g * MG; m < (g + 1) * MG; ++m) acc[m / S::FP][m % S::FP] = S::E::mma(fq[m / S::FP], fp[m % S::FP], acc[m / S::FP][m % S::FP]);
           __builtin_amdgcn_sched_barrier(0);

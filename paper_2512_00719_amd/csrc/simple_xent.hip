@@ -34,7 +34,8 @@ __device__ __forceinline__ Pair join(Pair a, Pair b) {
 
 struct Args {
   Operand hidden, weight;  // of the weights: the piece's rows
-  int k_bytes, np, nq;
+  int k_bytes;
+  Plan plan;
   float scale;
   const int32_t* targets;
   int64_t V, v0;           // whole vocabulary, the piece's first row
@@ -48,43 +49,53 @@ struct Args {
 };
 
 template <class S, bool DIRECT>
-__global__ __launch_bounds__(S::THREADS) void stats_kernel(Args a) {
-  __shared__ __align__(1024) unsigned char lds[S::LDS];
-  int tp, tq;
-  tile_of(blockIdx.x, a.np, a.nq, tp, tq);
-  const int64_t p0 = (int64_t)tp * S::BP, q0 = (int64_t)tq * S::BQ, T = a.hidden.rows;
+__device__ __forceinline__ void stats_tile(const Args& a, int64_t p0, int64_t q0, unsigned char* lds) {
+  const int64_t T = a.hidden.rows;
   typename S::Acc acc[S::FQ][S::FP];
   product<S, DIRECT>(a.hidden, a.weight, p0, q0, a.k_bytes, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
   const int64_t q1 = q0 + wq * S::FQ * 16 + (lane >> 4) * 4;
   const int left = (int)min((int64_t)S::BQ, a.V - q1);  // the lane's columns that exist
+  if (q0 + S::BQ > a.V) {
+#pragma unroll
+    for (int i = 0; i < S::FQ; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (i * 16 + e >= left) {
+#pragma unroll
+          for (int j = 0; j < S::FP; ++j) acc[i][j][e] = -INFINITY;  // (the scale is positive)
+        }
+  }
   Pair(*part)[S::BP] = reinterpret_cast<Pair(*)[S::BP]>(lds);
+  const float scale2 = a.scale * LOG2E;
 #pragma unroll
   for (int j = 0; j < S::FP; ++j) {
     const int pl = (wp * S::FP + j) * 16 + (lane & 15);
     const int64_t p = p0 + pl;
     const int64_t target = p < T ? (int64_t)a.targets[p] - q1 : -1;
+    if (target >= 0 && target < S::FQ * 16 && target < left) {  // (few tiles hold a token's target)
+#pragma unroll
+      for (int i = 0; i < S::FQ; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (target == i * 16 + e) a.at_target[p] = acc[i][j][e] * a.scale;
+    }
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < S::FQ; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float z = i * 16 + e < left ? acc[i][j][e] * a.scale : -INFINITY;
-        acc[i][j][e] = z;
-        m = fmaxf(m, z);
-        if (target == i * 16 + e && i * 16 + e < left) a.at_target[p] = z;
-      }
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     m = fmaxf(m, __shfl_xor(m, 32, 64));
-    const float base = m == -INFINITY ? 0.f : m;
+    const float base = m == -INFINITY ? 0.f : m * scale2;
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < S::FQ; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s += exp_of(acc[i][j][e] - base);
+      for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], scale2, -base));
     s += __shfl_xor(s, 16, 64);
     s += __shfl_xor(s, 32, 64);
-    if (lane < 16) part[wq][pl] = Pair{m, s};
+    if (lane < 16) part[wq][pl] = Pair{m * a.scale, s};
   }
   __syncthreads();
   for (int t = threadIdx.x; t < S::BP; t += S::THREADS) {
@@ -92,12 +103,17 @@ __global__ __launch_bounds__(S::THREADS) void stats_kernel(Args a) {
     Pair v = part[0][t];
 #pragma unroll
     for (int w = 1; w < S::NWQ; ++w) v = join(v, part[w][t]);
-    a.pairs[(int64_t)tq * T + p0 + t] = v;
+    a.pairs[q0 / S::BQ * T + p0 + t] = v;
   }
+}
+template <class S, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void stats_kernel(Args a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
+  tile_of<S>(a.plan, a.hidden.rows, [&](auto shape, int64_t p0, int64_t q0) { stats_tile<decltype(shape), DIRECT>(a, p0, q0, lds); });
 }
 
 // The tiles' pairs of 16 tokens a workgroup, by FIN_GROUPS groups of tiles.
-constexpr int FIN_T = 16, FIN_GROUPS = 64;
+constexpr int FIN_T = 16, FIN_GROUPS = 64, FIN_AHEAD = 8;
 __global__ __launch_bounds__(FIN_T * FIN_GROUPS) void finish_kernel(const Pair* pairs, int nq, int64_t T, int64_t V, const int32_t* targets,
                                                                     const float* at_target, float* loss, float* lse) {
   __shared__ Pair part[FIN_GROUPS][FIN_T];
@@ -105,8 +121,19 @@ __global__ __launch_bounds__(FIN_T * FIN_GROUPS) void finish_kernel(const Pair* 
   const int64_t t = (int64_t)blockIdx.x * FIN_T + lane;
   Pair v{-INFINITY, 0.f};
   if (t < T) {
-#pragma unroll 4
-    for (int q = grp; q < nq; q += FIN_GROUPS) v = join(v, pairs[(int64_t)q * T + t]);
+    for (int q0 = grp; q0 < nq; q0 += FIN_GROUPS * FIN_AHEAD) {
+      Pair x[FIN_AHEAD];
+#pragma unroll
+      for (int u = 0; u < FIN_AHEAD; ++u) {
+        const int q = q0 + u * FIN_GROUPS;
+        x[u] = q < nq ? pairs[(int64_t)q * T + t] : Pair{-INFINITY, 0.f};
+      }
+#pragma unroll
+      for (int n = FIN_AHEAD / 2; n > 0; n /= 2)
+#pragma unroll
+        for (int u = 0; u < n; ++u) x[u] = join(x[u], x[u + n]);
+      v = join(v, x[0]);
+    }
   }
   part[grp][lane] = v;
   for (int n = FIN_GROUPS / 2; n > 0; n /= 2) {
@@ -139,7 +166,8 @@ __global__ void clear_kernel(uint32_t* tops) { if (threadIdx.x < TOPS) tops[thre
 __device__ __forceinline__ void raise(uint32_t* top, float v) {  // the order of magnitudes' bits; the maximum does not depend on who comes first
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = __uint_as_float(max(__float_as_uint(v), (uint32_t)__shfl_xor((int)__float_as_uint(v), o, 64)));
-  if ((threadIdx.x & 63) == 0) atomicMax(top, __float_as_uint(v));
+  // (most find a larger one there already: thousands of atomics on one word would wait for each other)
+  if ((threadIdx.x & 63) == 0 && __float_as_uint(v) > __hip_atomic_load(top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(top, __float_as_uint(v));
 }
 // The larger magnitude, a NaN above all.
 __device__ __forceinline__ float larger(float a, float b) { return __uint_as_float(max(__float_as_uint(a) & 0x7FFFFFFFu, __float_as_uint(b) & 0x7FFFFFFFu)); }
@@ -190,16 +218,22 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
     if (lane == 0) a.tokens[t] = k;
     return;
   }
+  constexpr int AHEAD = 8;  // loads in flight
   float top = 0.f;
   const int64_t waves = ((int64_t)gridDim.x - a.token_wgs) * 4;
   for (int64_t v = ((int64_t)blockIdx.x - a.token_wgs) * 4 + wave; v < a.V; v += waves) {
     const uint16_t* w = a.weight + v * a.weight_stride;
-#pragma unroll 8
-    for (int64_t c = lane * VEC; c < a.D; c += 64 * VEC) {
-      float x[VEC];
-      load<uint16_t, VEC>(w + c, x);
+    for (int64_t c = lane * VEC; c < a.D; c += 64 * VEC * AHEAD) {
+      float x[AHEAD][VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) top = larger(top, x[e]);
+      for (int u = 0; u < AHEAD; ++u)
+        if (c + u * 64 * VEC < a.D) load<uint16_t, VEC>(w + c + u * 64 * VEC, x[u]);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (c + u * 64 * VEC < a.D) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) top = larger(top, x[u][e]);
+        }
     }
   }
   raise(a.tops + TOP_WEIGHTS, top);
@@ -209,11 +243,8 @@ __device__ __forceinline__ uint32_t f16_bits(float f) { return (uint32_t)__built
 
 // G of a tile, in both orders.  Columns behind the piece's last and tokens behind the last are zeros: sums run over them.
 template <class S, bool DIRECT>
-__global__ __launch_bounds__(S::THREADS) void g_kernel(Args a) {
-  __shared__ __align__(1024) unsigned char lds[S::LDS];
-  int tp, tq;
-  tile_of(blockIdx.x, a.np, a.nq, tp, tq);
-  const int64_t p0 = (int64_t)tp * S::BP, q0 = (int64_t)tq * S::BQ, T = a.hidden.rows;
+__device__ __forceinline__ void g_tile(const Args& a, int64_t p0, int64_t q0, unsigned char* lds) {
+  const int64_t T = a.hidden.rows;
   typename S::Acc acc[S::FQ][S::FP];
   product<S, DIRECT>(a.hidden, a.weight, p0, q0, a.k_bytes, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
@@ -222,22 +253,29 @@ __global__ __launch_bounds__(S::THREADS) void g_kernel(Args a) {
   const int left = (int)min((int64_t)S::BQ, a.weight.rows - q1);
   // A tile that LDS holds whole is turned there: two tokens of a column in a word, rows of 512 bytes whose 16-byte chunks are stored in an
   // order that spreads a store's eight rows over the banks.  (Stored by single values, the second order took 25 of a tile's 130 us.)
-  constexpr bool TURN = S::BP * S::BQ * 2 <= S::LDS && S::BP == 256;
-  auto place = [](int q, int chunk) { return q * (S::BP * 2) + ((chunk ^ (((q >> 2) & 3) * 2 + (q & 1) * 8)) << 4); };
+  constexpr bool TURN = S::BP * S::BQ * 2 <= S::LDS && S::BP >= 64;
+  auto place = [](int q, int chunk) { return q * (S::BP * 2) + ((chunk ^ ((((q >> 2) & 3) * 2 + (q & 1) * 8) & (S::BP / 8 - 1))) << 4); };
 #pragma unroll
   for (int j = 0; j < S::FP; ++j) {
     const int pl = (wp * S::FP + j) * 16 + (lane & 15);
     const int64_t p = p0 + pl;
     const Token k = p < T ? a.tokens[p] : Token{-1, 0.f, 1.f, 0.f};
     const int64_t target = (int64_t)k.y - a.v0 - q1;
+    const bool here = k.y >= 0 && target >= 0 && target < S::FQ * 16;
+    const float up = k.up;
 #pragma unroll
     for (int i = 0; i < S::FQ; ++i) {
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = exp_of(acc[i][j][e] * a.scale - k.lse);
+      if (here) {  // (few tiles hold a token's target)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (target == i * 16 + e) f[e] -= 1.f;
+      }
       uint32_t v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float pr = exp_of(acc[i][j][e] * a.scale - k.lse);
-        v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits((target == i * 16 + e ? pr - 1.f : pr) * k.up) : 0u;
-      }
+      for (int e = 0; e < 4; ++e) v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits(f[e] * up) : 0u;
       if (a.g && p < T) *reinterpret_cast<uint2*>(a.g + p * a.g_stride + q1 + i * 16) = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
       if constexpr (TURN) {
         if (a.gt) {
@@ -266,6 +304,11 @@ __global__ __launch_bounds__(S::THREADS) void g_kernel(Args a) {
         *reinterpret_cast<i32x4*>(a.gt + (q0 + q) * a.gt_stride + p0 + c * 8) = *reinterpret_cast<const i32x4*>(lds + place(q, c));
     }
   }
+}
+template <class S, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void g_kernel(Args a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
+  tile_of<S>(a.plan, a.hidden.rows, [&](auto shape, int64_t p0, int64_t q0) { g_tile<decltype(shape), DIRECT>(a, p0, q0, lds); });
 }
 
 // out[c][r] = in[r][c], from bfloat16 to 16-bit floats of 11 bits in range: rows behind the last and rows of tokens that take no part are zeros,
@@ -317,19 +360,16 @@ __global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* in, int6
 
 struct MulArgs {
   Operand p, q;
-  int k_bytes, k_split, np, nq;  // each of gridDim.y workgroups of a tile takes k_split bytes of k
+  int k_bytes, k_split;  // each of gridDim.y workgroups of a tile takes k_split bytes of k
   void* out;
+  Plan plan;
   int64_t stride, split_stride;
   int type, add, vec;
   const uint32_t* top;           // not null: the sums are brought back by from_range
 };
 // out[p][q] (+)= sum over k, in float32 or rounded once.
 template <class S>
-__global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
-  __shared__ __align__(1024) unsigned char lds[S::LDS];
-  int tp, tq;
-  tile_of(blockIdx.x, a.np, a.nq, tp, tq);
-  const int64_t p0 = (int64_t)tp * S::BP, q0 = (int64_t)tq * S::BQ;
+__device__ __forceinline__ void mul_tile(MulArgs a, int64_t p0, int64_t q0, unsigned char* lds) {
   const int k0 = blockIdx.y * a.k_split;
   a.p.p += k0;
   a.q.p += k0;
@@ -366,6 +406,11 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
   };
   if (a.type == SIMPLE_F32) put((float*)a.out);
   else put((uint16_t*)a.out);
+}
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
+  tile_of<S>(a.plan, a.p.rows, [&](auto shape, int64_t p0, int64_t q0) { mul_tile<decltype(shape)>(a, p0, q0, lds); });
 }
 
 // dH: the splits' sums, in order, times what G's rows and the weights' range lack; zeros for tokens that take no part.
@@ -444,9 +489,8 @@ void multiply(MulArgs a, int splits, hipStream_t st) {
   a.vec = rows_aligned(a.out, a.stride, type_bytes(a.type), 4 * type_bytes(a.type));
   shaped<F16>(a.p.rows, [&](auto shape) {
     using S = decltype(shape);
-    a.np = (int)ceil_div(a.p.rows, S::BP);
-    a.nq = (int)ceil_div(a.q.rows, S::BQ);
-    hipLaunchKernelGGL(mul_kernel<S>, dim3((unsigned)(a.np * a.nq), (unsigned)splits), dim3(S::THREADS), 0, st, a);
+    a.plan = plan<S>(a.p.rows, a.q.rows, splits == 1);
+    hipLaunchKernelGGL(mul_kernel<S>, dim3((unsigned)a.plan.grid, (unsigned)splits), dim3(S::THREADS), 0, st, a);
   });
 }
 
@@ -462,6 +506,7 @@ int check_sizes(int64_t T, int64_t V, int64_t D) {
   if (T < 0 || V <= 0 || D <= 0) return SIMPLE_EINVAL;
   return T > MAX_T || V > MAX_V || D > MAX_D ? SIMPLE_ECAPACITY : SIMPLE_OK;
 }
+bool good_scale(float s) { return s > 0.f && s <= 3.4e38f; }
 int64_t pairs_bytes(int64_t T, int64_t V) { return ((ceil_div(V, tile_q(T)) * T * (int64_t)sizeof(Pair) + 255) & ~(int64_t)255); }
 }  // namespace
 
@@ -475,7 +520,7 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
                            int64_t workspace_bytes, void* hip_stream) {
   const int rc = check_sizes(T, V, D);
   if (rc != SIMPLE_OK) return rc;
-  if (hidden_stride < D || weight_stride < D) return SIMPLE_EINVAL;
+  if (hidden_stride < D || weight_stride < D || !good_scale(logit_scale)) return SIMPLE_EINVAL;
   if (T == 0) return SIMPLE_OK;
   if (!hidden_dev || !weight_dev || !targets_dev || !loss_dev || !lse_dev) return SIMPLE_EINVAL;
   if (!workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
@@ -493,13 +538,12 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
   const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
   shaped<Bf16>(T, [&](auto shape) {
     using S = decltype(shape);
-    a.np = (int)ceil_div(T, S::BP);
-    a.nq = (int)ceil_div(V, S::BQ);
-    const dim3 grid((unsigned)((int64_t)a.np * a.nq)), block(S::THREADS);
+    a.plan = plan<S>(T, V);
+    const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
     if (dir) hipLaunchKernelGGL((stats_kernel<S, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((stats_kernel<S, false>), grid, block, 0, st, a);
   });
-  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)ceil_div(T, FIN_T)), dim3(FIN_T * FIN_GROUPS), 0, st, (const Pair*)a.pairs, a.nq, T, V, targets_dev,
+  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)ceil_div(T, FIN_T)), dim3(FIN_T * FIN_GROUPS), 0, st, (const Pair*)a.pairs, a.plan.nq, T, V, targets_dev,
                      (const float*)a.at_target, loss_dev, lse_dev);
   return launched();
 }
@@ -516,7 +560,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   const int rc = check_sizes(T, V, D);
   if (rc != SIMPLE_OK) return rc;
   if (hidden_stride < D || weight_stride < D || (dhidden_dev && dhidden_stride < D) || (dweight_dev && dweight_stride < D)) return SIMPLE_EINVAL;
-  if (!good_type(dweight_dtype)) return SIMPLE_EINVAL;
+  if (!good_type(dweight_dtype) || !good_scale(logit_scale)) return SIMPLE_EINVAL;
   if (T == 0) dhidden_dev = nullptr;
   if (!dhidden_dev && (!dweight_dev || (T == 0 && accumulate))) return SIMPLE_OK;
   hipStream_t st = (hipStream_t)hip_stream;
@@ -559,9 +603,8 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
       shaped<Bf16>(T, [&](auto shape) {
         using S = decltype(shape);
-        a.np = (int)ceil_div(T, S::BP);
-        a.nq = (int)ceil_div(n, S::BQ);
-        const dim3 grid((unsigned)((int64_t)a.np * a.nq)), block(S::THREADS);
+        a.plan = plan<S>(T, n);
+        const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
         if (dir) hipLaunchKernelGGL((g_kernel<S, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((g_kernel<S, false>), grid, block, 0, st, a);
       });
