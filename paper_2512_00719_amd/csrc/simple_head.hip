@@ -28,41 +28,49 @@ template <typename T, bool VEC> __device__ __forceinline__ void put4(T* to, int6
   }
 }
 
-template <class S, bool DIRECT, typename T, bool VEC>
-__device__ __forceinline__ void linear_int8_tile(const Args& a, int64_t p0, int64_t q0, unsigned char* lds) {
-  typename S::Acc acc[S::FQ][S::FP];
-  product<S, DIRECT>(a.tokens, a.weights, p0, q0, a.k_bytes, lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t p1 = p0 + wave % S::NWP * S::FP * 16 + (lane & 15), q1 = q0 + wave / S::NWP * S::FQ * 16 + (lane >> 4) * 4;
-  const int64_t V = a.weights.rows;
-  float ws[S::FQ][4];
-#pragma unroll
-  for (int i = 0; i < S::FQ; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) ws[i][e] = q1 + i * 16 + e < V ? a.w_scales[q1 + i * 16 + e] : 0.f;
-#pragma unroll
-  for (int j = 0; j < S::FP; ++j) {
-    const int64_t p = p1 + j * 16;
-    if (p >= a.tokens.rows) continue;
-    const float s = a.scales[p];
-    T* row = (T*)a.out + p * a.out_stride;
-#pragma unroll
-    for (int i = 0; i < S::FQ; ++i) {
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * s * ws[i][e];
-      put4<T, VEC>(row + q1 + i * 16, V - (q1 + i * 16), v);
-    }
-  }
-}
+template <class S> constexpr bool many = Cut<S>::CAN;
+
 template <class S, bool DIRECT, typename T, bool VEC>
 __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
   __shared__ __align__(1024) unsigned char lds[S::LDS];
-  tile_of<S>(a.plan, a.tokens.rows, [&](auto shape, int64_t p0, int64_t q0) { linear_int8_tile<decltype(shape), DIRECT, T, VEC>(a, p0, q0, lds); });
+  planned<S, DIRECT, many<S>>(a.tokens, a.weights, a.k_bytes, a.plan, lds, [&](auto shape, auto& acc, int64_t p0, int64_t q0) {
+    using R = decltype(shape);
+    const int lane = opaque_lane(), wave = threadIdx.x >> 6;
+    const int64_t p1 = p0 + wave % R::NWP * R::FP * 16 + (lane & 15), q1 = q0 + wave / R::NWP * R::FQ * 16 + (lane >> 4) * 4;
+    const int64_t V = a.weights.rows;
+    float ws[R::FQ][4];
+#pragma unroll
+    for (int i = 0; i < R::FQ; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ws[i][e] = a.w_scales[min(q1 + i * 16 + e, V - 1)];
+    float ts[R::FP];
+#pragma unroll
+    for (int j = 0; j < R::FP; ++j) ts[j] = a.scales[min(p1 + j * 16, a.tokens.rows - 1)];
+#pragma unroll
+    for (int i = 0; i < R::FQ; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) arrived_value(ws[i][e]);
+#pragma unroll
+    for (int j = 0; j < R::FP; ++j) arrived_value(ts[j]);
+#pragma unroll
+    for (int j = 0; j < R::FP; ++j) {
+      const int64_t p = p1 + j * 16;
+      if (p >= a.tokens.rows) continue;
+      const float s = ts[j];
+      T* row = (T*)a.out + p * a.out_stride;
+#pragma unroll
+      for (int i = 0; i < R::FQ; ++i) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * s * ws[i][e];
+        put4<T, VEC>(row + q1 + i * 16, V - (q1 + i * 16), v);
+      }
+    }
+  });
 }
 
 template <class S, bool DIRECT> void launch(Args a, hipStream_t st) {
-  a.plan = plan<S>(a.tokens.rows, a.weights.rows);
+  a.plan = plan<S, many<S>>(a.tokens.rows, a.weights.rows);
   const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
   if (a.out_type == SIMPLE_F32) {
     if (a.vec) hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float, true>), grid, block, 0, st, a);

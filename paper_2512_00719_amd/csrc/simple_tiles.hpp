@@ -97,35 +97,30 @@ __device__ __forceinline__ int place_of(int id, int n) {
   return x * per + min(x, more) + id / XCDS;
 }
 
-// A tile that fills a compute unit takes it alone, so that tiles run in rounds of CUS.  Tiles of a last round that is at most a quarter full are cut in
-// four along P instead, eight waves to each part, a compute unit to each: the round then takes about 0.35 of a whole one.
+// Tiles of 256 x 256 have a compute unit each: with MANY, as many workgroups as there are take them in rounds, one after the other, so that a workgroup's loads run
+// on from a tile to the next while the finished one is stored.  (Smaller tiles, several of them on a compute unit, are left to the dispatcher, one a
+// workgroup: taken in rounds, one token against 128,256 x 4096 int8 weights took 117 us, 92 so.)  Tiles of a last round that is at most a quarter full are cut in
+// four along P instead, eight waves to each part, a workgroup to each: the round then takes about 0.35 of a whole one.
+// (The lane as done() has it: hidden from the optimiser, which would otherwise keep what follows from it in registers through the products.)
+__device__ __forceinline__ int opaque_lane() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+template <typename T> __device__ __forceinline__ void arrived_value(T& v) { asm volatile("" : "+v"(v)); }
 template <class S> struct Cut {
   static constexpr bool CAN = S::BP == 256 && S::BQ == 256;
   using Part = Shape<typename S::E, CAN ? 64 : S::BP, S::BQ, CAN ? 1 : S::NWP, CAN ? 8 : S::NWQ, S::STAGES>;
 };
-struct Plan { int np, nq, whole, grid; };  // whole tiles, and workgroups in all
-template <class S> inline Plan plan(int64_t p_rows, int64_t q_rows, bool may_cut = true) {
-  Plan r{(int)ceil_div(p_rows, S::BP), (int)ceil_div(q_rows, S::BQ), 0, 0};
-  const int n = r.np * r.nq, last = n % CUS;
+struct Plan { int np, nq, whole, wgs, grid; };  // whole tiles, workgroups that take them, and workgroups in all
+template <class S, bool MANY> inline Plan plan(int64_t p_rows, int64_t q_rows, bool may_cut = true) {
+  Plan r{(int)ceil_div(p_rows, S::BP), (int)ceil_div(q_rows, S::BQ), 0, 0, 0};
+  const int n = r.np * r.nq, last = n % CUS, slots = MANY ? CUS : n;
   const bool cut = may_cut && Cut<S>::CAN && last > 0 && last * 4 <= CUS;
   r.whole = cut ? n - last : n;
-  r.grid = r.whole + (n - r.whole) * 4;
+  r.wgs = r.whole < slots ? r.whole : slots;
+  r.grid = r.wgs + (n - r.whole) * 4;
   return r;
-}
-// Calls f(shape, p0, q0) for the workgroup's tile or part of one.
-template <class S, typename F> __device__ __forceinline__ void tile_of(const Plan& r, int64_t p_rows, F&& f) {
-  int p, q;
-  if constexpr (Cut<S>::CAN) {
-    if ((int)blockIdx.x >= r.whole) {
-      const int i = place_of((int)blockIdx.x - r.whole, r.grid - r.whole);
-      tile_at(r.whole + i / 4, r.np, r.nq, p, q);
-      const int64_t p0 = (int64_t)p * S::BP + i % 4 * Cut<S>::Part::BP;
-      if (p0 < p_rows) f(typename Cut<S>::Part{}, p0, (int64_t)q * S::BQ);
-      return;
-    }
-  }
-  tile_at(place_of((int)blockIdx.x, r.whole), r.np, r.nq, p, q);
-  f(S{}, (int64_t)p * S::BP, (int64_t)q * S::BQ);
 }
 
 // 16 bytes of a row from byte `k` on, zeros behind its end; any alignment.
@@ -148,21 +143,48 @@ template <int BYTES> __device__ __forceinline__ i32x4 chunk_of(const unsigned ch
   return v;
 }
 
+// Rows of a tile on their way to LDS by to_lds().  Rows behind an operand's last repeat it (what they give is not stored).
+template <class S> struct Loader {
+  i32x4 res_p, res_q;
+  uint32_t off_p[S::LP], off_q[S::LQ];
+  int wave, chunk, row8, k_bytes;
+  __device__ __forceinline__ void to(const Operand& P, const Operand& Q, int64_t p0, int64_t q0) {
+    res_p = resource_of(P, p0, S::BP, k_bytes);
+    res_q = resource_of(Q, q0, S::BQ, k_bytes);
+    const int p_rows = (int)min((int64_t)S::BP, P.rows - p0), q_rows = (int)min((int64_t)S::BQ, Q.rows - q0);
+#pragma unroll
+    for (int i = 0; i < S::LP; ++i) off_p[i] = (uint32_t)min((wave + i * S::NW) % S::GP * 8 + row8, p_rows - 1) * (uint32_t)P.stride + chunk * 16;
+#pragma unroll
+    for (int i = 0; i < S::LQ; ++i) off_q[i] = (uint32_t)min((wave + i * S::NW) % S::GQ * 8 + row8, q_rows - 1) * (uint32_t)Q.stride + chunk * 16;
+  }
+  // load n of step s: the LP of P, then the LQ of Q
+  __device__ __forceinline__ void load(int s, uint32_t stage, int n) const {
+    const uint32_t k = (uint32_t)s * KB;
+    const bool behind = (int)k + chunk * 16 >= k_bytes;  // behind the row's end: an address behind the resource's, which reads as zeros
+    if (n < S::LP) to_lds(stage + (wave + n * S::NW) % S::GP * 1024, behind ? 0x80000000u : off_p[n], res_p, k);
+    else to_lds(stage + S::BP * KB + (wave + (n - S::LP) * S::NW) % S::GQ * 1024, behind ? 0x80000000u : off_q[n - S::LP], res_q, k);
+  }
+};
+
+// Forms tiles `tile(0)`, `tile(1)`, ... (which says whether there is one, and where; the first alone without MANY) and calls done(acc, p0, q0) for each.
+// With MANY the products come after done()'s code in a loop: a value that done() loads is to be used on each of its paths (arrived_value), or the
+// compiler waits for every load in flight when it gives the register to the products.
 // acc[i][j] of a lane: rows q0 + (wave along Q * FQ + i) * 16 + (lane >> 4) * 4 + 0..3 of Q against row p0 + (wave along P * FP + j) * 16 + (lane & 15) of P.
-// Rows behind an operand's last repeat it (what they give is not stored).  DIRECT: rows are staged by to_lds(), which
-// wants them 16-byte aligned with k_bytes a multiple of 16; else through registers, any alignment.
-template <class S, bool DIRECT>
-__device__ __forceinline__ void product(const Operand& P, const Operand& Q, int64_t p0, int64_t q0, int k_bytes, unsigned char* lds,
-                                        typename S::Acc (&acc)[S::FQ][S::FP]) {
+// DIRECT: rows are staged by to_lds(), which wants them 16-byte aligned with k_bytes a multiple of 16; else through registers,
+// any alignment.  `lds` are S::LDS bytes; done() must not write them with MANY, and without only behind a barrier of its own.
+template <class S, bool DIRECT, bool MANY, typename Tile, typename Done>
+__device__ __forceinline__ void products(const Operand& P, const Operand& Q, int k_bytes, unsigned char* lds, Tile&& tile, Done&& done) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % S::NWP, wq = wave / S::NWP;
   const int steps = (k_bytes + KB - 1) / KB;
   const int row8 = lane >> 3, chunk = (lane & 7) ^ row8;  // what a lane stages of its group of 8 rows
-  const int p_rows = (int)min((int64_t)S::BP, P.rows - p0), q_rows = (int)min((int64_t)S::BQ, Q.rows - q0);
+  typename S::Acc acc[S::FQ][S::FP];
+  auto clear = [&] {
 #pragma unroll
-  for (int i = 0; i < S::FQ; ++i)
+    for (int i = 0; i < S::FQ; ++i)
 #pragma unroll
-    for (int j = 0; j < S::FP; ++j) acc[i][j] = typename S::Acc{0, 0, 0, 0};
+      for (int j = 0; j < S::FP; ++j) acc[i][j] = typename S::Acc{0, 0, 0, 0};
+  };
   uint32_t at_p[2], at_q[2];  // the lane's place in the first fragment, for both halves of a step
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -188,114 +210,178 @@ __device__ __forceinline__ void product(const Operand& P, const Operand& Q, int6
         for (int j = 0; j < S::FP; ++j) acc[i][j] = S::E::mma(fq[i], fp[j], acc[i][j]);
     }
   };
+  int64_t p0, q0;
+  if (steps == 0) {
+    for (int n = 0; tile(n, p0, q0); ++n) {
+      clear();
+      done(acc, p0, q0);
+      if constexpr (!MANY) break;
+    }
+    return;
+  }
   if constexpr (DIRECT) {
-    const i32x4 res_p = resource_of(P, p0, S::BP, k_bytes), res_q = resource_of(Q, q0, S::BQ, k_bytes);
-    uint32_t off_p[S::LP], off_q[S::LQ];
-#pragma unroll
-    for (int i = 0; i < S::LP; ++i) off_p[i] = (uint32_t)min((wave + i * S::NW) % S::GP * 8 + row8, p_rows - 1) * (uint32_t)P.stride + chunk * 16;
-#pragma unroll
-    for (int i = 0; i < S::LQ; ++i) off_q[i] = (uint32_t)min((wave + i * S::NW) % S::GQ * 8 + row8, q_rows - 1) * (uint32_t)Q.stride + chunk * 16;
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-    // load n of step s: the LP of P, then the LQ of Q
-    auto load = [&](int s, int stage, int n) {
-      const uint32_t b = base + stage * S::STAGE, k = (uint32_t)s * KB;
-      const bool behind = (int)k + chunk * 16 >= k_bytes;  // behind the row's end: an address behind the resource's, which reads as zeros
-      if (n < S::LP) to_lds(b + (wave + n * S::NW) % S::GP * 1024, behind ? 0x80000000u : off_p[n], res_p, k);
-      else to_lds(b + S::BP * KB + (wave + (n - S::LP) * S::NW) % S::GQ * 1024, behind ? 0x80000000u : off_q[n - S::LP], res_q, k);
+    constexpr int NL = S::LP + S::LQ;
+    // the step that is loaded next: step ls of tile lt, if there is one
+    Loader<S> from;
+    from.wave = wave; from.chunk = chunk; from.row8 = row8; from.k_bytes = k_bytes;
+    int lt = 0, ls = 0;
+    bool more;
+    {
+      int64_t lp, lq;
+      more = tile(0, lp, lq);
+      if (!more) return;
+      from.to(P, Q, lp, lq);
+    }
+    auto onward = [&] {
+      if (++ls == steps) {
+        more = false;
+        if constexpr (MANY) {
+          ls = 0;
+          int64_t lp, lq;
+          more = tile(++lt, lp, lq);
+          if (more) from.to(P, Q, lp, lq);
+        }
+      }
     };
-    auto issue = [&](int s, int stage) {
+    auto issue = [&](int stage) {
 #pragma unroll
-      for (int n = 0; n < S::LP + S::LQ; ++n) load(s, stage, n);
+      for (int n = 0; n < NL; ++n) from.load(ls, base + stage * S::STAGE, n);
+      onward();
     };
     if constexpr (S::STAGES == 2) {
       // Bound by the matrix instructions.  A half's fragments are read while the half before is multiplied, and the barrier stands in the middle of a
       // step: there all of its fragments are in registers, the stage is free, and the step after has arrived.  Loads go out
       // one at a time between groups of products: eight in a row fill the memory pipeline's queue, and the wave waits there with its products (bfloat16
       // 8192 x 128,256 x 4096: 1.34 PFLOP/s so, 1.26 with the loads in front, 1.24 with neither).
-      constexpr int NF = S::FP + S::FQ, NL = S::LP + S::LQ, NM = S::FP * S::FQ, GROUPS = 8, MG = NM / GROUPS, RG = GROUPS - 2;
+      constexpr int NF = S::FP + S::FQ, NM = S::FP * S::FQ, GROUPS = 8, MG = NM / GROUPS, RG = GROUPS - 2;
       static_assert(NM % GROUPS == 0, "groups");
       i32x4 fp0[S::FP], fq0[S::FQ], fp1[S::FP], fq1[S::FQ];
-      auto half = [&](i32x4 (&fp)[S::FP], i32x4 (&fq)[S::FQ], bool next, int stage, int h, i32x4 (&np)[S::FP], i32x4 (&nq)[S::FQ], bool more, int s, int to) {
+      auto half = [&](i32x4 (&fp)[S::FP], i32x4 (&fq)[S::FQ], bool next, int stage, int h, i32x4 (&np)[S::FP], i32x4 (&nq)[S::FQ], bool ahead, uint32_t to) {
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
           if (next) {
 #pragma unroll
             for (int n = g * NF / RG; n < min(NF, (g + 1) * NF / RG); ++n) read(stage, h, n, np, nq);
           }
-          if (more) {
+          if (ahead) {
 #pragma unroll
-            for (int n = g * NL / GROUPS; n < (g + 1) * NL / GROUPS; ++n) load(s, to, n);
+            for (int n = g * NL / GROUPS; n < (g + 1) * NL / GROUPS; ++n) from.load(ls, to, n);
           }
 #pragma unroll
           for (int m = g * MG; m < (g + 1) * MG; ++m) acc[m / S::FP][m % S::FP] = S::E::mma(fq[m / S::FP], fp[m % S::FP], acc[m / S::FP][m % S::FP]);
           __builtin_amdgcn_sched_barrier(0);
         }
       };
-      if (steps > 0) {
-        issue(0, 0);
-        if (steps > 1) { issue(1, 1); arrived<NL>(); }
-        else arrived<0>();
-#pragma unroll
-        for (int n = 0; n < NF; ++n) read(0, 0, n, fp0, fq0);
-      }
-      for (int s = 0; s < steps; ++s) {
-        const bool next = s + 1 < steps;
-        half(fp0, fq0, true, s & 1, 1, fp1, fq1, false, 0, 0);
-        if (next) arrived<0>();
-        __builtin_amdgcn_sched_barrier(0);
-        half(fp1, fq1, next, (s + 1) & 1, 0, fp0, fq0, s + 2 < steps, s + 2, s & 1);
-      }
-      arrived<0>();  // (the caller may use the memory)
-      return;
-    }
-    // Bound by memory: more stages, all of a step's loads at once.
-#pragma unroll
-    for (int s = 0; s < S::STAGES - 1; ++s)
-      if (s < steps) issue(s, s);
-    int stage = 0;
-    for (int s = 0; s < steps; ++s) {
-      // the newest loads in flight are those of the steps behind this one
-      if (s + S::STAGES - 2 < steps) arrived<(S::STAGES - 2) * (S::LP + S::LQ)>();
+      issue(0);
+      const bool two = more;
+      if (two) { issue(1); arrived<NL>(); }
       else arrived<0>();
-      if (s + S::STAGES - 1 < steps) issue(s + S::STAGES - 1, stage == 0 ? S::STAGES - 1 : stage - 1);  // the stage of the step before: read by all
-      step(stage);
-      stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+      int stage = 0;
+      for (int n = 0; tile(n, p0, q0); ++n) {
+        clear();
+#pragma unroll
+        for (int f = 0; f < NF; ++f) read(stage, 0, f, fp0, fq0);
+        for (int s = 0; s < steps; ++s) {
+          half(fp0, fq0, true, stage, 1, fp1, fq1, false, 0);
+          arrived<0>();
+          __builtin_amdgcn_sched_barrier(0);
+          const bool ahead = more;
+          half(fp1, fq1, s + 1 < steps, stage ^ 1, 0, fp0, fq0, ahead, base + stage * S::STAGE);
+          if (ahead) onward();
+          stage ^= 1;
+        }
+        done(acc, p0, q0);
+        if constexpr (!MANY) break;
+      }
+    } else {
+      // Bound by memory: more stages, all of a step's loads at once.
+      int in_flight = 0;  // steps loaded and not yet multiplied
+      for (; in_flight < S::STAGES - 1 && more; ++in_flight) issue(in_flight);
+      int stage = 0;
+      for (int n = 0; tile(n, p0, q0); ++n) {
+        clear();
+        for (int s = 0; s < steps; ++s) {
+          // the newest loads in flight are those of the steps behind this one
+          if (in_flight == S::STAGES - 1) arrived<(S::STAGES - 2) * NL>();
+          else arrived<0>();
+          if (more) issue(stage == 0 ? S::STAGES - 1 : stage - 1);  // the stage of the step before: read by all
+          else --in_flight;
+          step(stage);
+          stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+        }
+        done(acc, p0, q0);
+        if constexpr (!MANY) break;
+      }
     }
-    arrived<0>();  // (the caller may use the memory)
   } else {
-    const unsigned char *row_p[S::LP], *row_q[S::LQ];
+    for (int n = 0; tile(n, p0, q0); ++n) {
+      const int p_rows = (int)min((int64_t)S::BP, P.rows - p0), q_rows = (int)min((int64_t)S::BQ, Q.rows - q0);
+      const unsigned char *row_p[S::LP], *row_q[S::LQ];
 #pragma unroll
-    for (int i = 0; i < S::LP; ++i) row_p[i] = P.p + (p0 + min((wave + i * S::NW) % S::GP * 8 + row8, p_rows - 1)) * P.stride;
+      for (int i = 0; i < S::LP; ++i) row_p[i] = P.p + (p0 + min((wave + i * S::NW) % S::GP * 8 + row8, p_rows - 1)) * P.stride;
 #pragma unroll
-    for (int i = 0; i < S::LQ; ++i) row_q[i] = Q.p + (q0 + min((wave + i * S::NW) % S::GQ * 8 + row8, q_rows - 1)) * Q.stride;
-    i32x4 v[S::LP + S::LQ];
-    auto fetch = [&](int s) {
-      const int64_t k = (int64_t)s * KB + chunk * 16;
+      for (int i = 0; i < S::LQ; ++i) row_q[i] = Q.p + (q0 + min((wave + i * S::NW) % S::GQ * 8 + row8, q_rows - 1)) * Q.stride;
+      i32x4 v[S::LP + S::LQ];
+      auto fetch = [&](int s) {
+        const int64_t k = (int64_t)s * KB + chunk * 16;
 #pragma unroll
-      for (int i = 0; i < S::LP; ++i) v[i] = chunk_of<S::E::BYTES>(row_p[i], k, k_bytes);
+        for (int i = 0; i < S::LP; ++i) v[i] = chunk_of<S::E::BYTES>(row_p[i], k, k_bytes);
 #pragma unroll
-      for (int i = 0; i < S::LQ; ++i) v[S::LP + i] = chunk_of<S::E::BYTES>(row_q[i], k, k_bytes);
-    };
-    auto put = [&](int stage) {
-      unsigned char* b = lds + stage * S::STAGE + lane * 16;
+        for (int i = 0; i < S::LQ; ++i) v[S::LP + i] = chunk_of<S::E::BYTES>(row_q[i], k, k_bytes);
+      };
+      auto put = [&](int stage) {
+        unsigned char* b = lds + stage * S::STAGE + lane * 16;
 #pragma unroll
-      for (int i = 0; i < S::LP; ++i) *reinterpret_cast<i32x4*>(b + (wave + i * S::NW) % S::GP * 1024) = v[i];
+        for (int i = 0; i < S::LP; ++i) *reinterpret_cast<i32x4*>(b + (wave + i * S::NW) % S::GP * 1024) = v[i];
 #pragma unroll
-      for (int i = 0; i < S::LQ; ++i) *reinterpret_cast<i32x4*>(b + S::BP * KB + (wave + i * S::NW) % S::GQ * 1024) = v[S::LP + i];
-    };
-    fetch(0);
-    put(0);
-    for (int s = 0; s < steps; ++s) {
-      __syncthreads();
-      if (s + 1 < steps) fetch(s + 1);
-      step(s & 1);
-      if (s + 1 < steps) put((s + 1) & 1);  // read last in the step before, ahead of the barrier
+        for (int i = 0; i < S::LQ; ++i) *reinterpret_cast<i32x4*>(b + S::BP * KB + (wave + i * S::NW) % S::GQ * 1024) = v[S::LP + i];
+      };
+      clear();
+      fetch(0);
+      __syncthreads();  // the tile before is read
+      put(0);
+      for (int s = 0; s < steps; ++s) {
+        __syncthreads();
+        if (s + 1 < steps) fetch(s + 1);
+        step(s & 1);
+        if (s + 1 < steps) put((s + 1) & 1);  // read last in the step before, ahead of the barrier
+      }
+      done(acc, p0, q0);
+      if constexpr (!MANY) break;
     }
-    __syncthreads();
   }
 }
 
-// Whether product<S, true> takes the operand: its resource's offsets stay below 2^31.
+// A workgroup's share of the plan: its tiles in rounds, or one part of a cut tile.  done(shape, acc, p0, q0).
+template <class S, bool DIRECT, bool MANY, typename Done>
+__device__ __forceinline__ void planned(const Operand& P, const Operand& Q, int k_bytes, const Plan& r, unsigned char* lds, Done&& done) {
+  if constexpr (Cut<S>::CAN) {
+    using Part = typename Cut<S>::Part;
+    if ((int)blockIdx.x >= r.wgs) {
+      const int i = place_of((int)blockIdx.x - r.wgs, r.grid - r.wgs);
+      products<Part, DIRECT, false>(P, Q, k_bytes, lds, [&](int n, int64_t& p0, int64_t& q0) {
+        int p, q;
+        tile_at(r.whole + i / 4, r.np, r.nq, p, q);
+        p0 = (int64_t)p * S::BP + i % 4 * Part::BP;
+        q0 = (int64_t)q * S::BQ;
+        return n == 0 && p0 < P.rows;
+      }, [&](auto& acc, int64_t p0, int64_t q0) { done(Part{}, acc, p0, q0); });
+      return;
+    }
+  }
+  products<S, DIRECT, MANY>(P, Q, k_bytes, lds, [&](int n, int64_t& p0, int64_t& q0) {
+    const int first = n * r.wgs, count = min(r.wgs, r.whole - first);
+    if ((int)blockIdx.x >= count) return false;
+    int p, q;
+    tile_at(first + place_of((int)blockIdx.x, count), r.np, r.nq, p, q);
+    p0 = (int64_t)p * S::BP;
+    q0 = (int64_t)q * S::BQ;
+    return true;
+  }, [&](auto& acc, int64_t p0, int64_t q0) { done(S{}, acc, p0, q0); });
+}
+
+// Whether products<S, true> takes the operand: its resource's offsets stay below 2^31.
 inline bool direct(const Operand& o, int64_t k_bytes) {
   return ((uintptr_t)o.p & 15u) == 0 && (o.stride & 15) == 0 && (k_bytes & 15) == 0 && o.stride <= ((int64_t)1 << 22) && k_bytes <= ((int64_t)1 << 30);
 }

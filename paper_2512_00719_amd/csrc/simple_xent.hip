@@ -48,12 +48,11 @@ struct Args {
   int64_t g_stride, gt_stride;
 };
 
-template <class S, bool DIRECT>
-__device__ __forceinline__ void stats_tile(const Args& a, int64_t p0, int64_t q0, unsigned char* lds) {
+template <class S> constexpr int stats_room = S::BP * S::NWQ * (int)sizeof(Pair);  // (a cut tile's parts need a half of it)
+template <class S>
+__device__ __forceinline__ void stats_of(const Args& a, typename S::Acc (&acc)[S::FQ][S::FP], int64_t p0, int64_t q0, unsigned char* room) {
   const int64_t T = a.hidden.rows;
-  typename S::Acc acc[S::FQ][S::FP];
-  product<S, DIRECT>(a.hidden, a.weight, p0, q0, a.k_bytes, lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
+  const int lane = opaque_lane(), wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
   const int64_t q1 = q0 + wq * S::FQ * 16 + (lane >> 4) * 4;
   const int left = (int)min((int64_t)S::BQ, a.V - q1);  // the lane's columns that exist
   if (q0 + S::BQ > a.V) {
@@ -66,7 +65,7 @@ __device__ __forceinline__ void stats_tile(const Args& a, int64_t p0, int64_t q0
           for (int j = 0; j < S::FP; ++j) acc[i][j][e] = -INFINITY;  // (the scale is positive)
         }
   }
-  Pair(*part)[S::BP] = reinterpret_cast<Pair(*)[S::BP]>(lds);
+  Pair(*part)[S::BP] = reinterpret_cast<Pair(*)[S::BP]>(room);  // (a tile has a barrier at least ahead of the next one's use)
   const float scale2 = a.scale * LOG2E;
 #pragma unroll
   for (int j = 0; j < S::FP; ++j) {
@@ -108,8 +107,9 @@ __device__ __forceinline__ void stats_tile(const Args& a, int64_t p0, int64_t q0
 }
 template <class S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void stats_kernel(Args a) {
-  __shared__ __align__(1024) unsigned char lds[S::LDS];
-  tile_of<S>(a.plan, a.hidden.rows, [&](auto shape, int64_t p0, int64_t q0) { stats_tile<decltype(shape), DIRECT>(a, p0, q0, lds); });
+  __shared__ __align__(1024) unsigned char lds[S::LDS + stats_room<S>];
+  planned<S, DIRECT, false>(a.hidden, a.weight, a.k_bytes, a.plan, lds,
+                     [&](auto shape, auto& acc, int64_t p0, int64_t q0) { stats_of<decltype(shape)>(a, acc, p0, q0, lds + S::LDS); });
 }
 
 // The tiles' pairs of 16 tokens a workgroup, by FIN_GROUPS groups of tiles.
@@ -242,19 +242,21 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
 __device__ __forceinline__ uint32_t f16_bits(float f) { return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)f); }
 
 // G of a tile, in both orders.  Columns behind the piece's last and tokens behind the last are zeros: sums run over them.
-template <class S, bool DIRECT>
-__device__ __forceinline__ void g_tile(const Args& a, int64_t p0, int64_t q0, unsigned char* lds) {
+template <class S>
+__device__ __forceinline__ void g_of(const Args& a, typename S::Acc (&acc)[S::FQ][S::FP], int64_t p0, int64_t q0, unsigned char* lds) {
   const int64_t T = a.hidden.rows;
-  typename S::Acc acc[S::FQ][S::FP];
-  product<S, DIRECT>(a.hidden, a.weight, p0, q0, a.k_bytes, lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
+  const int lane = opaque_lane(), wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
   const int ql = wq * S::FQ * 16 + (lane >> 4) * 4;  // the lane's first column in the tile
   const int64_t q1 = q0 + ql;
   const int left = (int)min((int64_t)S::BQ, a.weight.rows - q1);
-  // A tile that LDS holds whole is turned there: two tokens of a column in a word, rows of 512 bytes whose 16-byte chunks are stored in an
-  // order that spreads a store's eight rows over the banks.  (Stored by single values, the second order took 25 of a tile's 130 us.)
-  constexpr bool TURN = S::BP * S::BQ * 2 <= S::LDS && S::BP >= 64;
-  auto place = [](int q, int chunk) { return q * (S::BP * 2) + ((chunk ^ ((((q >> 2) & 3) * 2 + (q & 1) * 8) & (S::BP / 8 - 1))) << 4); };
+  // The second order of a tile that LDS holds whole is made there: two tokens of a column in a word, rows of all the tile's tokens whose 16-byte
+  // chunks are stored in an order that spreads a store's eight rows over the banks.  (Stored by single values, it took 25 of a 256 x 256 tile's
+  // 130 us; a quarter of the tile at a time, beside the next tile's loads, 6 more than so.)
+  constexpr bool TURN = S::STAGES == 2;
+  static_assert(!TURN || S::BP * S::BQ * 2 <= S::LDS, "room");
+  constexpr int CHUNKS = S::BP / 8;  // of a row
+  auto place = [](int q, int chunk) { return q * (S::BP * 2) + ((chunk ^ ((((q >> 2) & 3) * 2 + (q & 1) * 8) & (CHUNKS - 1))) << 4); };
+  if constexpr (TURN) __syncthreads();  // (the last step is read)
 #pragma unroll
   for (int j = 0; j < S::FP; ++j) {
     const int pl = (wp * S::FP + j) * 16 + (lane & 15);
@@ -262,7 +264,6 @@ __device__ __forceinline__ void g_tile(const Args& a, int64_t p0, int64_t q0, un
     const Token k = p < T ? a.tokens[p] : Token{-1, 0.f, 1.f, 0.f};
     const int64_t target = (int64_t)k.y - a.v0 - q1;
     const bool here = k.y >= 0 && target >= 0 && target < S::FQ * 16;
-    const float up = k.up;
 #pragma unroll
     for (int i = 0; i < S::FQ; ++i) {
       float f[4];
@@ -275,7 +276,7 @@ __device__ __forceinline__ void g_tile(const Args& a, int64_t p0, int64_t q0, un
       }
       uint32_t v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits(f[e] * up) : 0u;
+      for (int e = 0; e < 4; ++e) v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits(f[e] * k.up) : 0u;
       if (a.g && p < T) *reinterpret_cast<uint2*>(a.g + p * a.g_stride + q1 + i * 16) = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
       if constexpr (TURN) {
         if (a.gt) {
@@ -284,8 +285,7 @@ __device__ __forceinline__ void g_tile(const Args& a, int64_t p0, int64_t q0, un
 #pragma unroll
           for (int e = 0; e < 4; e += 2) {
             const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? v[e] : v[e + 1]), 0xB1, 0xF, 0xF, true);  // quad_perm 1 0 3 2
-            const int q = ql + i * 16 + e + odd;
-            *reinterpret_cast<uint32_t*>(lds + place(q, pl >> 3) + (pl & 6) * 2) = odd ? other | v[e + 1] << 16 : v[e] | other << 16;
+            *reinterpret_cast<uint32_t*>(lds + place(ql + i * 16 + e + odd, pl >> 3) + (pl & 6) * 2) = odd ? other | v[e + 1] << 16 : v[e] | other << 16;
           }
         }
       } else if (a.gt && p < a.gt_stride) {
@@ -297,7 +297,6 @@ __device__ __forceinline__ void g_tile(const Args& a, int64_t p0, int64_t q0, un
   if constexpr (TURN) {
     if (!a.gt) return;
     __syncthreads();
-    constexpr int CHUNKS = S::BP / 8;  // of a row
     for (int n = threadIdx.x; n < S::BQ * CHUNKS; n += S::THREADS) {
       const int q = n / CHUNKS, c = n % CHUNKS;
       if (p0 + c * 8 < a.gt_stride)  // (a multiple of 16)
@@ -308,7 +307,8 @@ __device__ __forceinline__ void g_tile(const Args& a, int64_t p0, int64_t q0, un
 template <class S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void g_kernel(Args a) {
   __shared__ __align__(1024) unsigned char lds[S::LDS];
-  tile_of<S>(a.plan, a.hidden.rows, [&](auto shape, int64_t p0, int64_t q0) { g_tile<decltype(shape), DIRECT>(a, p0, q0, lds); });
+  planned<S, DIRECT, false>(a.hidden, a.weight, a.k_bytes, a.plan, lds,
+                            [&](auto shape, auto& acc, int64_t p0, int64_t q0) { g_of<decltype(shape)>(a, acc, p0, q0, lds); });
 }
 
 // out[c][r] = in[r][c], from bfloat16 to 16-bit floats of 11 bits in range: rows behind the last and rows of tokens that take no part are zeros,
@@ -369,23 +369,24 @@ struct MulArgs {
 };
 // out[p][q] (+)= sum over k, in float32 or rounded once.
 template <class S>
-__device__ __forceinline__ void mul_tile(MulArgs a, int64_t p0, int64_t q0, unsigned char* lds) {
+__global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
+  __shared__ __align__(1024) unsigned char lds[S::LDS];
   const int k0 = blockIdx.y * a.k_split;
   a.p.p += k0;
   a.q.p += k0;
-  typename S::Acc acc[S::FQ][S::FP];
-  product<S, true>(a.p, a.q, p0, q0, max(0, min(a.k_split, a.k_bytes - k0)), lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t p1 = p0 + wave % S::NWP * S::FP * 16 + (lane & 15), q1 = q0 + wave / S::NWP * S::FQ * 16 + (lane >> 4) * 4;
   const float back = a.top ? from_range(*a.top) : 1.f;
+  planned<S, true, Cut<S>::CAN>(a.p, a.q, max(0, min(a.k_split, a.k_bytes - k0)), a.plan, lds, [&](auto shape, auto& acc, int64_t p0, int64_t q0) {
+  using R = decltype(shape);
+  const int lane = opaque_lane(), wave = threadIdx.x >> 6;
+  const int64_t p1 = p0 + wave % R::NWP * R::FP * 16 + (lane & 15), q1 = q0 + wave / R::NWP * R::FQ * 16 + (lane >> 4) * 4;
   auto put = [&](auto* out) {
     using T = std::remove_pointer_t<decltype(out)>;
 #pragma unroll
-    for (int j = 0; j < S::FP; ++j) {
+    for (int j = 0; j < R::FP; ++j) {
       if (p1 + j * 16 >= a.p.rows) continue;
       T* row = out + blockIdx.y * a.split_stride + (p1 + j * 16) * a.stride;
 #pragma unroll
-      for (int i = 0; i < S::FQ; ++i) {
+      for (int i = 0; i < R::FQ; ++i) {
         const int64_t q = q1 + i * 16;
         float v[4] = {acc[i][j][0] * back, acc[i][j][1] * back, acc[i][j][2] * back, acc[i][j][3] * back};
         if (a.vec && q + 4 <= a.q.rows) {
@@ -406,11 +407,7 @@ __device__ __forceinline__ void mul_tile(MulArgs a, int64_t p0, int64_t q0, unsi
   };
   if (a.type == SIMPLE_F32) put((float*)a.out);
   else put((uint16_t*)a.out);
-}
-template <class S>
-__global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
-  __shared__ __align__(1024) unsigned char lds[S::LDS];
-  tile_of<S>(a.plan, a.p.rows, [&](auto shape, int64_t p0, int64_t q0) { mul_tile<decltype(shape)>(a, p0, q0, lds); });
+  });
 }
 
 // dH: the splits' sums, in order, times what G's rows and the weights' range lack; zeros for tokens that take no part.
@@ -489,7 +486,7 @@ void multiply(MulArgs a, int splits, hipStream_t st) {
   a.vec = rows_aligned(a.out, a.stride, type_bytes(a.type), 4 * type_bytes(a.type));
   shaped<F16>(a.p.rows, [&](auto shape) {
     using S = decltype(shape);
-    a.plan = plan<S>(a.p.rows, a.q.rows, splits == 1);
+    a.plan = plan<S, Cut<S>::CAN>(a.p.rows, a.q.rows, splits == 1);
     hipLaunchKernelGGL(mul_kernel<S>, dim3((unsigned)a.plan.grid, (unsigned)splits), dim3(S::THREADS), 0, st, a);
   });
 }
@@ -538,7 +535,7 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
   const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
   shaped<Bf16>(T, [&](auto shape) {
     using S = decltype(shape);
-    a.plan = plan<S>(T, V);
+    a.plan = plan<S, false>(T, V);
     const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
     if (dir) hipLaunchKernelGGL((stats_kernel<S, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((stats_kernel<S, false>), grid, block, 0, st, a);
@@ -603,7 +600,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
       shaped<Bf16>(T, [&](auto shape) {
         using S = decltype(shape);
-        a.plan = plan<S>(T, n);
+        a.plan = plan<S, false>(T, n);
         const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
         if (dir) hipLaunchKernelGGL((g_kernel<S, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((g_kernel<S, false>), grid, block, 0, st, a);
