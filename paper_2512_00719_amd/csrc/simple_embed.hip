@@ -18,7 +18,7 @@ using namespace vocab;
 
 constexpr int WG = 256;
 constexpr int RD = 4;              // rows in flight per thread of the lookup
-constexpr int TILE = 2048;         // tokens a workgroup of the sort
+constexpr int TILE = 1024;         // tokens a workgroup of the sort
 constexpr int BITS = 9, BINS = 1 << BITS;
 constexpr int CHUNK = 32;          // sorted places a workgroup of the sums
 constexpr int ROUNDS = TILE / WG;  // a wave's tokens, 64 at a time
@@ -52,23 +52,35 @@ __global__ __launch_bounds__(WG) void lookup_kernel(const int32_t* ids, const T*
 // ---- zeros ----
 struct Fill {
   unsigned char* p;
-  int64_t rows, row_bytes, stride_bytes;
+  int64_t rows, row_bytes, stride_bytes, first;  // first: the share's number in the table
 };
-// Workgroup `at` of `n`: its share of the rows, in pieces of 16 bytes where the address allows it, else of 2.
-__device__ __forceinline__ void fill_share(const Fill& f, int64_t at, int64_t n) {
-  typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-  const bool whole = f.row_bytes == f.stride_bytes;  // one long row
-  const int64_t rows = whole ? 1 : f.rows, bytes = whole ? f.rows * f.row_bytes : f.row_bytes;
-  for (int64_t r = whole ? 0 : at; r < rows; r += whole ? 1 : n) {
-    unsigned char* p = f.p + r * f.stride_bytes;
-    const int64_t head = min(bytes, (int64_t)((16u - (uint32_t)(uintptr_t)p) & 15u)), body = (bytes - head) / 16;
-    const int64_t first = whole ? at * WG : 0, step = whole ? n * WG : WG;
-    for (int64_t i = first + threadIdx.x; i < body; i += step) *reinterpret_cast<v4u*>(p + head + 16 * i) = v4u{0u, 0u, 0u, 0u};
-    if (!whole || at == 0) {
-      for (int64_t i = 2 * threadIdx.x; i < head; i += 2 * WG) *reinterpret_cast<uint16_t*>(p + i) = 0;
-      for (int64_t i = head + 16 * body + 2 * threadIdx.x; i < bytes; i += 2 * WG) *reinterpret_cast<uint16_t*>(p + i) = 0;
-    }
+// Zeros are written beside the sort's kernels, a share of the table by each: the sort leaves most of the chip idle.  Workgroup `at` of a
+// kernel takes one store of 16 bytes a thread: 525 MB at 6.7 TB/s so, 5.9 with pieces of 16 KB, 5.0 to 5.5 with 64 KB, 4.4 with workgroups
+// that go on to other pieces.  The stores are non-temporal, which leaves what the sums read next in the caches (16,384 tokens of 2048 bfloat16 values: sums
+// 23 us, 36 behind ordinary stores).
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void fill_piece(unsigned char* p, int64_t bytes) {  // 2-byte aligned
+  const int64_t head = min(bytes, (int64_t)((16u - (uint32_t)(uintptr_t)p) & 15u)), body = (bytes - head) / 16;
+  v4u* q = reinterpret_cast<v4u*>(p + head);
+  const v4u zero = {0u, 0u, 0u, 0u};
+  for (int64_t i = threadIdx.x; i < body; i += blockDim.x) __builtin_nontemporal_store(zero, q + i);
+  for (int64_t k = 2 * threadIdx.x; k < head; k += 2 * blockDim.x) *reinterpret_cast<uint16_t*>(p + k) = 0;
+  for (int64_t k = head + 16 * body + 2 * threadIdx.x; k < bytes; k += 2 * blockDim.x) *reinterpret_cast<uint16_t*>(p + k) = 0;
+}
+__device__ __forceinline__ void fill_share(const Fill& f, int64_t at) {
+  const int64_t piece = 16 * (int64_t)blockDim.x;
+  at += f.first;
+  if (f.row_bytes == f.stride_bytes) {  // one long row
+    const int64_t all = f.rows * f.row_bytes, b = at * piece;
+    if (b < all) fill_piece(f.p + b, min(piece, all - b));
+  } else {
+    const int64_t each = max((int64_t)1, piece / f.row_bytes), r1 = min(f.rows, (at + 1) * each);
+    for (int64_t r = at * each; r < r1; ++r) fill_piece(f.p + r * f.stride_bytes, f.row_bytes);
   }
+}
+inline int64_t fill_workgroups(const Fill& f, int threads) {
+  const int64_t piece = 16 * (int64_t)threads;
+  return f.row_bytes == f.stride_bytes ? ceil_div(f.rows * f.row_bytes, piece) : ceil_div(f.rows, std::max<int64_t>(1, piece / f.row_bytes));
 }
 
 // ---- sort: stable, BITS bits of the id a pass, from the lowest ----
@@ -86,7 +98,7 @@ __device__ __forceinline__ int32_t key_of(const Sort& s, int64_t i) {
 }
 
 __global__ __launch_bounds__(WG) void count_kernel(Sort s, Fill f) {
-  if ((int)blockIdx.x >= s.tiles) { fill_share(f, (int)blockIdx.x - s.tiles, (int)gridDim.x - s.tiles); return; }
+  if ((int)blockIdx.x >= s.tiles) { fill_share(f, (int)blockIdx.x - s.tiles); return; }
   __shared__ int32_t cnt[BINS];
   for (int i = threadIdx.x; i < BINS; i += WG) cnt[i] = 0;
   __syncthreads();
@@ -99,38 +111,19 @@ __global__ __launch_bounds__(WG) void count_kernel(Sort s, Fill f) {
   for (int i = threadIdx.x; i < BINS; i += WG) s.counts[(int64_t)blockIdx.x * BINS + i] = cnt[i];
 }
 
-// A tile's tokens go to their places: behind all tokens of lower digits, those of the same digit in earlier tiles, in earlier waves
-// of the tile, in earlier rounds of the wave and in lower lanes.
-__global__ __launch_bounds__(WG) void place_kernel(Sort s, Fill f) {
-  if ((int)blockIdx.x >= s.tiles) { fill_share(f, (int)blockIdx.x - s.tiles, (int)gridDim.x - s.tiles); return; }
-  constexpr int NW = WG / 64;
-  __shared__ int32_t cnt[NW][BINS];
-  __shared__ int32_t scan[NW];
+// Places of a tile's tokens by one digit: behind all tokens of lower digits, those of the same digit in earlier tiles (`ahead`, of `all`), in earlier
+// waves of the tile, in earlier rounds of the wave and in lower lanes.  Thread t's digits are 2t and 2t + 1 below BINS.  Each wave holds R rounds of 64
+// consecutive tokens, `n` of the tile's exist; place[k] is round k's.
+template <int NW, int R>
+__device__ __forceinline__ void places(const int32_t (&key)[R], int n, int shift, bool alone, const int32_t (&ahead)[2], int32_t (&all)[2], int32_t (*cnt)[BINS],
+                                       int32_t* scan, int32_t (&place)[R]) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  for (int i = tid; i < NW * BINS; i += WG) (&cnt[0][0])[i] = 0;
-  // counts of the tiles ahead, and of all
-  int32_t ahead[2] = {0, 0}, all[2] = {0, 0};
-  if (s.tiles > 1) {
-#pragma unroll 4
-    for (int t = 0; t < s.tiles; ++t) {
-      const int2 c = *reinterpret_cast<const int2*>(s.counts + (int64_t)t * BINS + 2 * tid);
-      all[0] += c.x; all[1] += c.y;
-      if (t < (int)blockIdx.x) { ahead[0] += c.x; ahead[1] += c.y; }
-    }
-  }
+  for (int i = tid; i < NW * BINS; i += 64 * NW) (&cnt[0][0])[i] = 0;
   __syncthreads();
-  const int64_t w0 = (int64_t)blockIdx.x * TILE + wave * (ROUNDS * 64);
-  int32_t key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
 #pragma unroll
-  for (int k = 0; k < ROUNDS; ++k) {
-    const int64_t i = w0 + k * 64 + lane;
-    key[k] = i < s.n ? key_of(s, i) : 0;
-    pos[k] = i < s.n ? (s.pos_in ? s.pos_in[i] : (int32_t)i) : 0;
-  }
-#pragma unroll
-  for (int k = 0; k < ROUNDS; ++k) {
-    const bool in = w0 + k * 64 + lane < s.n;
-    const uint32_t d = ((uint32_t)key[k] >> s.shift) & (BINS - 1);
+  for (int k = 0; k < R; ++k) {
+    const bool in = wave * (R * 64) + k * 64 + lane < n;
+    const uint32_t d = ((uint32_t)key[k] >> shift) & (BINS - 1);
     uint64_t same = __ballot(in);
 #pragma unroll
     for (int b = 0; b < BITS; ++b) {
@@ -140,14 +133,16 @@ __global__ __launch_bounds__(WG) void place_kernel(Sort s, Fill f) {
     const int first = in ? __ffsll((unsigned long long)same) - 1 : lane;
     int32_t old = 0;
     if (in && lane == first) old = atomicAdd(&cnt[wave][d], (int32_t)__popcll(same));
-    rank[k] = __shfl(old, first, 64) + (int32_t)__popcll(same & ((1ull << lane) - 1ull));
+    place[k] = __shfl(old, first, 64) + (int32_t)__popcll(same & ((1ull << lane) - 1ull));
   }
   __syncthreads();
-  // first place of each digit for this tile, then for each of its waves
   int32_t own[2] = {0, 0};
+  const bool digits = 2 * tid < BINS;
+  if (digits) {
 #pragma unroll
-  for (int w = 0; w < NW; ++w) { own[0] += cnt[w][2 * tid]; own[1] += cnt[w][2 * tid + 1]; }
-  if (s.tiles == 1) { all[0] = own[0]; all[1] = own[1]; }
+    for (int w = 0; w < NW; ++w) { own[0] += cnt[w][2 * tid]; own[1] += cnt[w][2 * tid + 1]; }
+  }
+  if (alone) { all[0] = own[0]; all[1] = own[1]; }
   int32_t pre = all[0] + all[1];
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -157,22 +152,82 @@ __global__ __launch_bounds__(WG) void place_kernel(Sort s, Fill f) {
   if (lane == 63) scan[wave] = pre;
   __syncthreads();
   for (int w = 0; w < wave; ++w) pre += scan[w];
-  int32_t base[2] = {pre - all[0] - all[1] + ahead[0], pre - all[1] + ahead[1]};
+  if (digits) {
+    int32_t base[2] = {pre - all[0] - all[1] + ahead[0], pre - all[1] + ahead[1]};
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    const int32_t c0 = cnt[w][2 * tid], c1 = cnt[w][2 * tid + 1];
-    cnt[w][2 * tid] = base[0]; cnt[w][2 * tid + 1] = base[1];
-    base[0] += c0; base[1] += c1;
+    for (int w = 0; w < NW; ++w) {
+      const int32_t c0 = cnt[w][2 * tid], c1 = cnt[w][2 * tid + 1];
+      cnt[w][2 * tid] = base[0]; cnt[w][2 * tid + 1] = base[1];
+      base[0] += c0; base[1] += c1;
+    }
   }
   __syncthreads();
 #pragma unroll
+  for (int k = 0; k < R; ++k) place[k] += cnt[wave][((uint32_t)key[k] >> shift) & (BINS - 1)];
+}
+
+__global__ __launch_bounds__(WG) void place_kernel(Sort s, Fill f) {
+  if ((int)blockIdx.x >= s.tiles) { fill_share(f, (int)blockIdx.x - s.tiles); return; }
+  __shared__ int32_t cnt[WG / 64][BINS];
+  __shared__ int32_t scan[WG / 64];
+  static_assert(2 * WG >= BINS, "two digits a thread");
+  const int tid = threadIdx.x;
+  int32_t ahead[2] = {0, 0}, all[2] = {0, 0};  // counts of the tiles ahead, and of all
+#pragma unroll 4
+  for (int t = 0; t < s.tiles; ++t) {
+    const int2 c = *reinterpret_cast<const int2*>(s.counts + (int64_t)t * BINS + 2 * tid);
+    all[0] += c.x; all[1] += c.y;
+    if (t < (int)blockIdx.x) { ahead[0] += c.x; ahead[1] += c.y; }
+  }
+  const int64_t w0 = (int64_t)blockIdx.x * TILE + (tid >> 6) * (ROUNDS * 64) + (tid & 63);
+  int32_t key[ROUNDS], pos[ROUNDS], place[ROUNDS];
+#pragma unroll
   for (int k = 0; k < ROUNDS; ++k) {
-    if (w0 + k * 64 + lane < s.n) {
-      const int32_t to = cnt[wave][((uint32_t)key[k] >> s.shift) & (BINS - 1)] + rank[k];
-      s.key_out[to] = key[k];
-      s.pos_out[to] = pos[k];
+    const int64_t i = w0 + k * 64;
+    key[k] = i < s.n ? key_of(s, i) : 0;
+    pos[k] = i < s.n ? (s.pos_in ? s.pos_in[i] : (int32_t)i) : 0;
+  }
+  places<WG / 64, ROUNDS>(key, (int)min((int64_t)TILE, s.n - (int64_t)blockIdx.x * TILE), s.shift, false, ahead, all, cnt, scan, place);
+#pragma unroll
+  for (int k = 0; k < ROUNDS; ++k) {
+    if (w0 + k * 64 < s.n) {
+      s.key_out[place[k]] = key[k];
+      s.pos_out[place[k]] = pos[k];
     }
   }
+}
+
+// The whole sort of up to FEW tokens by one workgroup, which passes them through LDS from digit to digit (5 us for 1605 tokens; as kernels of their own
+// the four steps took 16).
+constexpr int FEW_WG = 1024, FEW = 4096, FEW_ROUNDS = FEW / FEW_WG;
+__global__ __launch_bounds__(FEW_WG) void sort_few_kernel(Sort s, int passes, Fill f) {
+  if (blockIdx.x > 0 || s.n == 0) { fill_share(f, (int)blockIdx.x - (s.n > 0)); return; }
+  __shared__ int32_t cnt[FEW_WG / 64][BINS];
+  __shared__ int32_t scan[FEW_WG / 64];
+  __shared__ int2 held[FEW];
+  const int w0 = (threadIdx.x >> 6) * (FEW_ROUNDS * 64) + (threadIdx.x & 63), n = (int)s.n;
+  int32_t key[FEW_ROUNDS], pos[FEW_ROUNDS], place[FEW_ROUNDS];
+#pragma unroll
+  for (int k = 0; k < FEW_ROUNDS; ++k) {
+    key[k] = w0 + k * 64 < n ? key_of(s, w0 + k * 64) : 0;
+    pos[k] = w0 + k * 64;
+  }
+  for (int p = 0; p < passes; ++p) {
+    const int32_t ahead[2] = {0, 0};
+    int32_t all[2] = {0, 0};
+    places<FEW_WG / 64, FEW_ROUNDS>(key, n, p * BITS, true, ahead, all, cnt, scan, place);
+    __syncthreads();  // (what was held is read)
+#pragma unroll
+    for (int k = 0; k < FEW_ROUNDS; ++k)
+      if (w0 + k * 64 < n) held[place[k]] = int2{key[k], pos[k]};
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < FEW_ROUNDS; ++k)
+      if (w0 + k * 64 < n) { key[k] = held[w0 + k * 64].x; pos[k] = held[w0 + k * 64].y; }
+  }
+#pragma unroll
+  for (int k = 0; k < FEW_ROUNDS; ++k)
+    if (w0 + k * 64 < n) { s.key_out[w0 + k * 64] = key[k]; s.pos_out[w0 + k * 64] = pos[k]; }
 }
 
 // ---- sums ----
@@ -206,7 +261,7 @@ __global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
   for (int i = threadIdx.x; i < CHUNK + 2; i += blockDim.x) {
     const int64_t at = s0 + i - 1;
     key[i] = at >= 0 && at < s.n ? s.key[at] : -1;
-    if (i < m) pos[i] = s.pos[s0 + i];
+    if (i < CHUNK) pos[i] = s.pos[s0 + (i < m ? i : 0)];
   }
   __syncthreads();
   const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
@@ -221,12 +276,11 @@ __global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
   for (int i0 = 0; i0 < m; i0 += AHEAD) {
     float v[AHEAD][VEC];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (i0 + u < m && key[1 + i0 + u] < s.V) load<T, VEC>(d + pos[i0 + u] * s.dout_stride, v[u]);
+    for (int u = 0; u < AHEAD; ++u) load<T, VEC>(d + pos[i0 + u] * s.dout_stride, v[u]);  // (places behind the last hold the first one's token)
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int i = i0 + u;
-      if (i >= m || key[1 + i] >= s.V) break;
+      if (i >= m || key[1 + i] >= s.V) return;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
       if (key[1 + i] != key[2 + i]) {  // the row's last token
@@ -357,21 +411,29 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
   hipStream_t st = (hipStream_t)hip_stream;
   unsigned char* ws = (unsigned char*)workspace_dev;
   const int64_t eo = type_bytes(table_dtype), ei = type_bytes(dtype);
-  const Fill zeros{(unsigned char*)dtable_dev, V, D * eo, dtable_stride * eo}, nothing{};
-  // the zeros are written beside the first kernel of the sort
-  const int64_t fill_bytes = V * D * eo, fill_wgs = accumulate ? 0 : std::min<int64_t>(2048, std::max<int64_t>(1, fill_bytes / (16 * WG * 4)));
   Sort s{ids_dev, nullptr, (int32_t*)(ws + L.key[0]), (int32_t*)(ws + L.pos[0]), (int32_t*)(ws + L.counts), T, V, L.tiles, 0};
-  int64_t fill_left = fill_wgs;
-  for (int p = 0; p < (T > 0 ? L.passes : 1); ++p) {
-    if (L.tiles > 1) {
-      hipLaunchKernelGGL(count_kernel, dim3((unsigned)(L.tiles + fill_left)), dim3(WG), 0, st, s, fill_left ? zeros : nothing);
-      fill_left = 0;
-    }
-    hipLaunchKernelGGL(place_kernel, dim3((unsigned)(L.tiles + fill_left)), dim3(WG), 0, st, s, fill_left ? zeros : nothing);
-    fill_left = 0;
+  Fill zeros{(unsigned char*)dtable_dev, V, D * eo, dtable_stride * eo, 0};
+  if (T <= FEW) {
+    const int64_t shares = accumulate ? 0 : fill_workgroups(zeros, FEW_WG);
+    hipLaunchKernelGGL(sort_few_kernel, dim3((unsigned)(shares + (T > 0))), dim3(FEW_WG), 0, st, s, L.passes, zeros);
     s.key_in = s.key_out; s.pos_in = s.pos_out;
-    s.key_out = (int32_t*)(ws + L.key[(p + 1) & 1]); s.pos_out = (int32_t*)(ws + L.pos[(p + 1) & 1]);
-    s.shift += BITS;
+  } else {
+    const int kernels = 2 * L.passes;
+    const int64_t shares = accumulate ? 0 : fill_workgroups(zeros, WG);
+    int kernel = 0;
+    auto beside = [&](auto* f) {  // the kernel's share of the zeros, behind its own workgroups
+      zeros.first = shares * kernel / kernels;
+      const int64_t n = shares * (kernel + 1) / kernels - zeros.first;
+      ++kernel;
+      hipLaunchKernelGGL(f, dim3((unsigned)(L.tiles + n)), dim3(WG), 0, st, s, zeros);
+    };
+    for (int p = 0; p < L.passes; ++p) {
+      beside(count_kernel);
+      beside(place_kernel);
+      s.key_in = s.key_out; s.pos_in = s.pos_out;
+      s.key_out = (int32_t*)(ws + L.key[(p + 1) & 1]); s.pos_out = (int32_t*)(ws + L.pos[(p + 1) & 1]);
+      s.shift += BITS;
+    }
   }
   if (T == 0) return launched();
   Sums m{s.key_in, s.pos_in, dout_dev, dout_stride, T, V, D, scale, dtable_dev, dtable_stride, accumulate, (float*)(ws + L.partial)};

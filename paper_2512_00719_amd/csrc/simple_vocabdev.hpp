@@ -42,7 +42,7 @@ inline int64_t type_bytes(int dtype) { return dtype == SIMPLE_F32 ? 4 : 2; }
 inline bool rows_aligned(const void* p, int64_t stride, int64_t esz, int64_t to) {
   return p == nullptr || (((uintptr_t)p & (uintptr_t)(to - 1)) == 0 && ((stride * esz) & (to - 1)) == 0);
 }
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int launched() { return hipGetLastError() == hipSuccess ? SIMPLE_OK : SIMPLE_EDEVICE; }
 
 }  // namespace vocab

@@ -221,19 +221,24 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   constexpr int AHEAD = 8;  // loads in flight
   float top = 0.f;
   const int64_t waves = ((int64_t)gridDim.x - a.token_wgs) * 4;
-  for (int64_t v = ((int64_t)blockIdx.x - a.token_wgs) * 4 + wave; v < a.V; v += waves) {
-    const uint16_t* w = a.weight + v * a.weight_stride;
-    for (int64_t c = lane * VEC; c < a.D; c += 64 * VEC * AHEAD) {
+  const bool whole = a.weight_stride == a.D;  // one long row, taken in pieces of what a wave has in flight
+  constexpr int64_t PIECE = 64 * VEC * AHEAD;
+  const int64_t n = whole ? ceil_div(a.V * a.D, PIECE) : a.V;
+  for (int64_t v = ((int64_t)blockIdx.x - a.token_wgs) * 4 + wave; v < n; v += waves) {
+    const uint16_t* w = a.weight + (whole ? v * PIECE : v * a.weight_stride);
+    const int64_t end = whole ? min(PIECE, a.V * a.D - v * PIECE) : a.D;
+    for (int64_t c = lane * VEC; c < end; c += PIECE) {
       float x[AHEAD][VEC];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u)
-        if (c + u * 64 * VEC < a.D) load<uint16_t, VEC>(w + c + u * 64 * VEC, x[u]);
+      for (int u = 0; u < AHEAD; ++u) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][e] = 0.f;
+        if (c + u * 64 * VEC < end) load<uint16_t, VEC>(w + c + u * 64 * VEC, x[u]);
+      }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
-        if (c + u * 64 * VEC < a.D) {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) top = larger(top, x[u][e]);
-        }
+        for (int e = 0; e < VEC; ++e) top = larger(top, x[u][e]);
     }
   }
   raise(a.tops + TOP_WEIGHTS, top);
@@ -410,19 +415,46 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
   });
 }
 
-// dH: the splits' sums, in order, times what G's rows and the weights' range lack; zeros for tokens that take no part.
-__global__ __launch_bounds__(256) void hidden_kernel(const float* sums, int splits, int64_t T, int64_t D, const Token* tokens, const uint32_t* top,
-                                                     uint16_t* out, int64_t stride) {
+// dH: the splits' sums, in an order that depends on their number alone, times what G's rows and the weights' range lack; zeros for tokens that
+// take no part.  HID_GROUPS threads share a column group's splits where there are several.
+constexpr int HID_GROUPS = 4;
+template <int VEC>
+__global__ __launch_bounds__(64 * HID_GROUPS) void hidden_kernel(const float* sums, int splits, int64_t T, int64_t D, const Token* tokens, const uint32_t* top,
+                                                                 uint16_t* out, int64_t stride) {
+  __shared__ float part[HID_GROUPS][64 * VEC];
   const int64_t t = blockIdx.x;
   const Token k = tokens[t];
   const float m = k.rest * from_range(*top);
-  for (int64_t c = threadIdx.x; c < D; c += 256) {
-    float v = 0.f;
-    if (k.y >= 0) {
-#pragma unroll 4
-      for (int s = 0; s < splits; ++s) v += sums[((int64_t)s * T + t) * D + c];
+  const bool shared_out = splits > 1;
+  const int lane = threadIdx.x & 63, grp = threadIdx.x >> 6;
+  const int64_t c = shared_out ? ((int64_t)blockIdx.y * 64 + lane) * VEC : ((int64_t)blockIdx.y * (64 * HID_GROUPS) + threadIdx.x) * VEC;
+  float v[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) v[e] = 0.f;
+  if (c < D && k.y >= 0) {
+    const float* p = sums + t * D + c;
+#pragma unroll 8
+    for (int s = shared_out ? grp : 0; s < splits; s += HID_GROUPS) {
+      float x[VEC];
+      load<float, VEC>(p + (int64_t)s * T * D, x);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] += x[e];
     }
-    out[t * stride + c] = to_bf16(k.y >= 0 ? v * m : 0.f);
+  }
+  if (shared_out) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) part[grp][lane * VEC + e] = v[e];
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int g = 1; g < HID_GROUPS; ++g)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] += part[g][lane * VEC + e];
+  }
+  if (c < D) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = k.y >= 0 ? v[e] * m : 0.f;
+    store<uint16_t, VEC>(out + t * stride + c, v);
   }
 }
 
@@ -436,6 +468,7 @@ template <class E, typename F> void shaped(int64_t T, F&& f) {
 }
 int64_t tile_q(int64_t T) { return T <= 64 ? 64 : T <= 128 ? 128 : 256; }
 
+constexpr int SHORT_K = 4 * KB;
 constexpr int64_t PIECE = (int64_t)1 << 27;   // values of G kept at a time (256 MB in each order)
 constexpr int64_t ROUND = 256;                // a piece's rows: a multiple of every tile
 constexpr int64_t MOST_ROWS = (int64_t)1 << 20;  // rows of G stay within what a buffer resource spans
@@ -484,7 +517,8 @@ void transpose(const uint16_t* in, int64_t stride, int64_t rows, int64_t cols, u
 void multiply(MulArgs a, int splits, hipStream_t st) {
   a.k_split = (int)(ceil_div(ceil_div(a.k_bytes, splits), KB) * KB);
   a.vec = rows_aligned(a.out, a.stride, type_bytes(a.type), 4 * type_bytes(a.type));
-  shaped<F16>(a.p.rows, [&](auto shape) {
+  // (Few steps of k, as dW of few tokens has: a tile is mostly stored, and two smaller ones on a compute unit do so in turn.)
+  shaped<F16>(a.k_bytes <= SHORT_K ? std::min<int64_t>(a.p.rows, 128) : a.p.rows, [&](auto shape) {
     using S = decltype(shape);
     a.plan = plan<S, Cut<S>::CAN>(a.p.rows, a.q.rows, splits == 1);
     hipLaunchKernelGGL(mul_kernel<S>, dim3((unsigned)a.plan.grid, (unsigned)splits), dim3(S::THREADS), 0, st, a);
@@ -632,8 +666,14 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       multiply(m, 1, st);
     }
   }
-  if (dhidden_dev)
-    hipLaunchKernelGGL(hidden_kernel, dim3((unsigned)T), dim3(256), 0, st, (const float*)(ws + L.sums), L.splits, T, D, tokens,
-                       tops + TOP_WEIGHTS, (uint16_t*)dhidden_dev, dhidden_stride);
+  if (dhidden_dev) {
+    auto hidden = [&](auto kernel, int vec) {
+      const int64_t columns = (int64_t)64 * vec * (L.splits > 1 ? 1 : HID_GROUPS);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)ceil_div(D, columns)), dim3(64 * HID_GROUPS), 0, st, (const float*)(ws + L.sums), L.splits, T, D,
+                         (const Token*)tokens, (const uint32_t*)(tops + TOP_WEIGHTS), (uint16_t*)dhidden_dev, dhidden_stride);
+    };
+    if (D % 4 == 0 && rows_aligned(dhidden_dev, dhidden_stride, 2, 8)) hidden(hidden_kernel<4>, 4);
+    else hidden(hidden_kernel<1>, 1);
+  }
   return launched();
 }
