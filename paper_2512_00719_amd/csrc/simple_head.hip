@@ -13,7 +13,7 @@ struct Args {
   Operand tokens, weights;
   int k_bytes, out_type;
   Plan plan;
-  bool vec;             // groups of four outputs may be stored together
+  bool vec;             // groups of 16 bytes of the output may be stored together
   const float *scales, *w_scales;
   void* out;
   int64_t out_stride;
@@ -55,15 +55,29 @@ __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
 #pragma unroll
     for (int j = 0; j < R::FP; ++j) {
       const int64_t p = p1 + j * 16;
-      if (p >= a.tokens.rows) continue;
       const float s = ts[j];
       T* row = (T*)a.out + p * a.out_stride;
+      if constexpr (VEC && sizeof(T) == 2 && R::FQ % 2 == 0) {
+        const int g = lane >> 4;
+        const int64_t q2 = q1 - g * 4 + 16 * (g / 2) + 8 * (g % 2);
 #pragma unroll
-      for (int i = 0; i < R::FQ; ++i) {
-        float v[4];
+        for (int i = 0; i < R::FQ; i += 2) {
+          uint2 x[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * s * ws[i][e];
-        put4<T, VEC>(row + q1 + i * 16, V - (q1 + i * 16), v);
+          for (int h = 0; h < 2; ++h)
+            x[h] = uint2{two_bf16((float)acc[i + h][j][0] * s * ws[i + h][0], (float)acc[i + h][j][1] * s * ws[i + h][1]),
+                         two_bf16((float)acc[i + h][j][2] * s * ws[i + h][2], (float)acc[i + h][j][3] * s * ws[i + h][3])};
+          eight_of(x[0], x[1]);
+          if (p < a.tokens.rows) put8((uint16_t*)row + q2 + i * 16, true, V - (q2 + i * 16), uint4{x[0].x, x[0].y, x[1].x, x[1].y});
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < R::FQ; ++i) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * s * ws[i][e];
+          if (p < a.tokens.rows) put4<T, VEC>(row + q1 + i * 16, V - (q1 + i * 16), v);
+        }
       }
     }
   });
@@ -104,7 +118,7 @@ extern "C" int simple_linear_int8(const int8_t* codes_dev, int64_t code_stride, 
   if (ceil_div(T, 16) * ceil_div(V, 64) > (int64_t)0x7FFFFFFF) return SIMPLE_ECAPACITY;
   const int64_t e = type_bytes(out_dtype);
   Args a{{(const unsigned char*)codes_dev, code_stride, T}, {(const unsigned char*)w_codes_dev, w_code_stride, V}, (int)K, out_dtype, Plan{},
-         rows_aligned(out_dev, out_stride, e, 4 * e), scales_dev, w_scales_dev, out_dev, out_stride};
+         rows_aligned(out_dev, out_stride, e, 16), scales_dev, w_scales_dev, out_dev, out_stride};
   hipStream_t st = (hipStream_t)hip_stream;
   if (direct(a.tokens, K) && direct(a.weights, K)) launch_for<true>(a, st);
   else launch_for<false>(a, st);

@@ -50,6 +50,11 @@ struct Operand {
 // The wave's 64 lanes write 1 KB from `lds` on in lane order: 8 rows of a step.  Nothing here is seen by the compiler's own count of loads
 // in flight; arrived() below waits for them, and no register is written.
 __device__ __forceinline__ void to_lds(uint32_t lds, uint32_t offset, i32x4 resource, uint32_t k) {
+  // (scalar operands, whatever register the optimiser has kept them in)
+  lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
+  k = (uint32_t)__builtin_amdgcn_readfirstlane((int)k);
+  resource = i32x4{__builtin_amdgcn_readfirstlane(resource.x), __builtin_amdgcn_readfirstlane(resource.y), __builtin_amdgcn_readfirstlane(resource.z),
+                   __builtin_amdgcn_readfirstlane(resource.w)};
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(resource), "s"(k) : "memory");
 }
 // All but the `N` newest of this wave's loads have arrived, and those of the workgroup's other waves; what the waves read of LDS before is in

@@ -17,6 +17,7 @@ __device__ __forceinline__ uint16_t to_bf16(float f) {
   if ((b & 0x7FFFFFFFu) > 0x7F800000u) return (uint16_t)((b >> 16) | 0x40u);
   return (uint16_t)((b + 0x7FFFu + ((b >> 16) & 1u)) >> 16);
 }
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) { return (uint32_t)to_bf16(a) | (uint32_t)to_bf16(b) << 16; }
 template <typename T> __device__ __forceinline__ T down(float f);
 template <> __device__ __forceinline__ float down<float>(float f) { return f; }
 template <> __device__ __forceinline__ uint16_t down<uint16_t>(float f) { return to_bf16(f); }
@@ -33,6 +34,31 @@ template <typename T, int VEC> __device__ __forceinline__ void store(T* p, const
 #pragma unroll
   for (int i = 0; i < VEC; ++i) g.v[i] = down<T>(in[i]);
   *reinterpret_cast<Group<T, VEC>*>(p) = g;
+}
+
+// A lane of a product's tile holds four consecutive 16-bit values (two words) of a row, its row's other 16-lane groups the next ones, and the values
+// 16 further on are in the next fragment.  `a` and `b` are two such fragments: afterwards the lane holds eight consecutive values, `a` then `b`, at
+// 16 * (group / 2) + 8 * (group % 2) from the first fragment's start, so that a store writes 64 bytes of each of 16 rows instead of 32.
+__device__ __forceinline__ void eight_of(uint2& a, uint2& b) {
+  auto swap = [](uint32_t& x, uint32_t& y) {
+    const auto h = __builtin_amdgcn_permlane32_swap(x, y, false, false);  // x's upper half against y's lower
+    const auto q = __builtin_amdgcn_permlane16_swap(h[0], h[1], false, false);  // x's odd sixteens against y's even
+    x = q[0];
+    y = q[1];
+  };
+  swap(a.x, b.x);
+  swap(a.y, b.y);
+}
+
+// The first n of eight 16-bit values, together where `to` is 16-byte aligned.
+__device__ __forceinline__ void put8(uint16_t* to, bool aligned, int64_t n, uint4 v) {
+  if (aligned && n >= 8) *reinterpret_cast<uint4*>(to) = v;
+  else {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) to[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+  }
 }
 
 // ---- host side ----

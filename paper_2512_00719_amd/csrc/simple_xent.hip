@@ -161,14 +161,6 @@ __device__ __forceinline__ float to_range(uint32_t top) {
 __device__ __forceinline__ float from_range(uint32_t top) { return 1.f / to_range(top); }
 enum { TOP_STATES = 0, TOP_WEIGHTS = 1, TOPS = 2 };
 
-__global__ void clear_kernel(uint32_t* tops) { if (threadIdx.x < TOPS) tops[threadIdx.x] = 0u; }
-
-__device__ __forceinline__ void raise(uint32_t* top, float v) {  // the order of magnitudes' bits; the maximum does not depend on who comes first
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = __uint_as_float(max(__float_as_uint(v), (uint32_t)__shfl_xor((int)__float_as_uint(v), o, 64)));
-  // (most find a larger one there already: thousands of atomics on one word would wait for each other)
-  if ((threadIdx.x & 63) == 0 && __float_as_uint(v) > __hip_atomic_load(top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(top, __float_as_uint(v));
-}
 // The larger magnitude, a NaN above all.
 __device__ __forceinline__ float larger(float a, float b) { return __uint_as_float(max(__float_as_uint(a) & 0x7FFFFFFFu, __float_as_uint(b) & 0x7FFFFFFFu)); }
 
@@ -179,19 +171,31 @@ struct PrepareArgs {
   const float *lse, *dloss;
   float scale;
   Token* tokens;
-  uint32_t* tops;
+  float* partial;  // a workgroup's largest magnitude each
   int token_wgs;
 };
+// The largest magnitude of a workgroup of NW waves.
+template <int NW> __device__ __forceinline__ float top_of(float v, float* part) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = larger(v, __shfl_xor(v, o, 64));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = part[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) v = larger(v, part[w]);
+  return v;
+}
 // The first workgroups: a wave a token, its logit at the target once more (for the power of two alone, so its order of summation does not matter)
 // and its largest state.  The rest: the weights' largest magnitude, rows in turn.
 template <int VEC>
 __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
+  __shared__ float part[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float most = 0.f;
   if ((int)blockIdx.x < a.token_wgs) {
     const int64_t t = (int64_t)blockIdx.x * 4 + wave;
-    if (t >= a.T) return;
-    const int32_t y = a.targets[t];
-    const float dl = a.dloss[t];
+    const int32_t y = t < a.T ? a.targets[t] : -1;
+    const float dl = t < a.T ? a.dloss[t] : 0.f;
     const bool on = y >= 0 && y < a.V && dl != 0.f;
     Token k{-1, 0.f, 1.f, 0.f};
     if (on) {
@@ -210,12 +214,14 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
       // below that is noise, and must not be scaled beyond the type's range, 4 times the row's aim
       const float lse = a.lse[t], left = -expm1f(dot * a.scale - lse);
       const float noise = 5.9604645e-8f * (sqrtf((float)a.D) * sizes * fabsf(a.scale) + fabsf(lse) + 1.f);
-      const float most = left < noise ? noise : left;
-      const int e = (most < 1.f ? ilogbf(most) + 1 : 0) - 14;
+      const float aim = left < noise ? noise : left;
+      const int e = (aim < 1.f ? ilogbf(aim) + 1 : 0) - 14;
       k = Token{y, lse, ldexpf(1.f, -e), dl * a.scale * ldexpf(1.f, e)};
-      raise(a.tops + TOP_STATES, larger(top * k.rest, 0.f));
+      most = top * k.rest;
     }
-    if (lane == 0) a.tokens[t] = k;
+    if (t < a.T && lane == 0) a.tokens[t] = k;
+    most = top_of<4>(most, part);
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = most;
     return;
   }
   constexpr int AHEAD = 8;  // loads in flight
@@ -241,7 +247,16 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
         for (int e = 0; e < VEC; ++e) top = larger(top, x[u][e]);
     }
   }
-  raise(a.tops + TOP_WEIGHTS, top);
+  top = top_of<4>(top, part);
+  if (threadIdx.x == 0) a.partial[blockIdx.x] = top;
+}
+// (By atomics on two words instead, thousands of workgroups waited for each other: 102 MB of weights took 120 us, 30 so.)
+__global__ __launch_bounds__(1024) void tops_kernel(const float* partial, int token_wgs, int wgs, uint32_t* tops) {
+  __shared__ float part[2][16];
+  float v[2] = {0.f, 0.f};
+  for (int i = threadIdx.x; i < wgs; i += 1024) v[i >= token_wgs] = larger(v[i >= token_wgs], partial[i]);
+  const float states = top_of<16>(v[0], part[0]), weights = top_of<16>(v[1], part[1]);
+  if (threadIdx.x == 0) { tops[TOP_STATES] = __float_as_uint(states); tops[TOP_WEIGHTS] = __float_as_uint(weights); }
 }
 
 __device__ __forceinline__ uint32_t f16_bits(float f) { return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)f); }
@@ -269,33 +284,48 @@ __device__ __forceinline__ void g_of(const Args& a, typename S::Acc (&acc)[S::FQ
     const Token k = p < T ? a.tokens[p] : Token{-1, 0.f, 1.f, 0.f};
     const int64_t target = (int64_t)k.y - a.v0 - q1;
     const bool here = k.y >= 0 && target >= 0 && target < S::FQ * 16;
+    constexpr int PAIR = S::FQ % 2 == 0 ? 2 : 1;
 #pragma unroll
-    for (int i = 0; i < S::FQ; ++i) {
-      float f[4];
+    for (int i0 = 0; i0 < S::FQ; i0 += PAIR) {
+      uint2 word[PAIR];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f[e] = exp_of(acc[i][j][e] * a.scale - k.lse);
-      if (here) {  // (few tiles hold a token's target)
+      for (int n = 0; n < PAIR; ++n) {
+        const int i = i0 + n;
+        float f[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (target == i * 16 + e) f[e] -= 1.f;
-      }
-      uint32_t v[4];
+        for (int e = 0; e < 4; ++e) f[e] = exp_of(acc[i][j][e] * a.scale - k.lse);
+        if (here) {  // (few tiles hold a token's target)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits(f[e] * k.up) : 0u;
-      if (a.g && p < T) *reinterpret_cast<uint2*>(a.g + p * a.g_stride + q1 + i * 16) = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
-      if constexpr (TURN) {
-        if (a.gt) {
-          // of each pair of columns the even lane takes the first for both tokens, the odd one the second
-          const bool odd = lane & 1;
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? v[e] : v[e + 1]), 0xB1, 0xF, 0xF, true);  // quad_perm 1 0 3 2
-            *reinterpret_cast<uint32_t*>(lds + place(ql + i * 16 + e + odd, pl >> 3) + (pl & 6) * 2) = odd ? other | v[e + 1] << 16 : v[e] | other << 16;
-          }
+          for (int e = 0; e < 4; ++e)
+            if (target == i * 16 + e) f[e] -= 1.f;
         }
-      } else if (a.gt && p < a.gt_stride) {
+        uint32_t v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) a.gt[(q1 + i * 16 + e) * a.gt_stride + p] = (uint16_t)v[e];
+        for (int e = 0; e < 4; ++e) v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits(f[e] * k.up) : 0u;
+        word[n] = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
+        if constexpr (TURN) {
+          if (a.gt) {
+            // of each pair of columns the even lane takes the first for both tokens, the odd one the second
+            const bool odd = lane & 1;
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+              const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)(odd ? v[e] : v[e + 1]), 0xB1, 0xF, 0xF, true);  // quad_perm 1 0 3 2
+              *reinterpret_cast<uint32_t*>(lds + place(ql + i * 16 + e + odd, pl >> 3) + (pl & 6) * 2) = odd ? other | v[e + 1] << 16 : v[e] | other << 16;
+            }
+          }
+        } else if (a.gt && p < a.gt_stride) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) a.gt[(q1 + i * 16 + e) * a.gt_stride + p] = (uint16_t)v[e];
+        }
+      }
+      if (a.g) {
+        if constexpr (PAIR == 2) {
+          eight_of(word[0], word[1]);
+          const int g = lane >> 4;
+          if (p < T) *reinterpret_cast<uint4*>(a.g + p * a.g_stride + q1 - g * 4 + 16 * (g / 2) + 8 * (g % 2) + i0 * 16) = uint4{word[0].x, word[0].y, word[1].x, word[1].y};
+        } else if (p < T) {
+          *reinterpret_cast<uint2*>(a.g + p * a.g_stride + q1 + i0 * 16) = word[0];
+        }
       }
     }
   }
@@ -366,14 +396,14 @@ __global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* in, int6
 struct MulArgs {
   Operand p, q;
   int k_bytes, k_split;  // each of gridDim.y workgroups of a tile takes k_split bytes of k
-  void* out;
   Plan plan;
+  void* out;
   int64_t stride, split_stride;
-  int type, add, vec;
+  bool vec;                      // rows are 16-byte aligned
   const uint32_t* top;           // not null: the sums are brought back by from_range
 };
 // out[p][q] (+)= sum over k, in float32 or rounded once.
-template <class S>
+template <class S, typename T, bool ADD>
 __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
   __shared__ __align__(1024) unsigned char lds[S::LDS];
   const int k0 = blockIdx.y * a.k_split;
@@ -381,37 +411,44 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
   a.q.p += k0;
   const float back = a.top ? from_range(*a.top) : 1.f;
   planned<S, true, Cut<S>::CAN>(a.p, a.q, max(0, min(a.k_split, a.k_bytes - k0)), a.plan, lds, [&](auto shape, auto& acc, int64_t p0, int64_t q0) {
-  using R = decltype(shape);
-  const int lane = opaque_lane(), wave = threadIdx.x >> 6;
-  const int64_t p1 = p0 + wave % R::NWP * R::FP * 16 + (lane & 15), q1 = q0 + wave / R::NWP * R::FQ * 16 + (lane >> 4) * 4;
-  auto put = [&](auto* out) {
-    using T = std::remove_pointer_t<decltype(out)>;
+    using R = decltype(shape);
+    const int lane = opaque_lane(), wave = threadIdx.x >> 6, g = lane >> 4;
+    const int64_t p1 = p0 + wave % R::NWP * R::FP * 16 + (lane & 15), q1 = q0 + wave / R::NWP * R::FQ * 16;
+    constexpr int PAIR = sizeof(T) == 2 && !ADD && R::FQ % 2 == 0 ? 2 : 1;
 #pragma unroll
     for (int j = 0; j < R::FP; ++j) {
-      if (p1 + j * 16 >= a.p.rows) continue;
-      T* row = out + blockIdx.y * a.split_stride + (p1 + j * 16) * a.stride;
+      const bool in = p1 + j * 16 < a.p.rows;
+      T* row = (T*)a.out + blockIdx.y * a.split_stride + (p1 + j * 16) * a.stride;
 #pragma unroll
-      for (int i = 0; i < R::FQ; ++i) {
-        const int64_t q = q1 + i * 16;
-        float v[4] = {acc[i][j][0] * back, acc[i][j][1] * back, acc[i][j][2] * back, acc[i][j][3] * back};
-        if (a.vec && q + 4 <= a.q.rows) {
-          if (a.add) {
-            float o[4];
-            load<T, 4>(row + q, o);
+      for (int i = 0; i < R::FQ; i += PAIR) {
+        if constexpr (PAIR == 2) {
+          uint2 x[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += o[e];
-          }
-          store<T, 4>(row + q, v);
+          for (int h = 0; h < 2; ++h)
+            x[h] = uint2{two_bf16(acc[i + h][j][0] * back, acc[i + h][j][1] * back), two_bf16(acc[i + h][j][2] * back, acc[i + h][j][3] * back)};
+          eight_of(x[0], x[1]);
+          const int64_t q = q1 + i * 16 + 16 * (g / 2) + 8 * (g % 2);
+          if (in) put8((uint16_t*)row + q, a.vec, a.q.rows - q, uint4{x[0].x, x[0].y, x[1].x, x[1].y});
         } else {
+          const int64_t q = q1 + i * 16 + g * 4;
+          float v[4] = {acc[i][j][0] * back, acc[i][j][1] * back, acc[i][j][2] * back, acc[i][j][3] * back};
+          if (in && a.vec && q + 4 <= a.q.rows) {
+            if constexpr (ADD) {
+              float o[4];
+              load<T, 4>(row + q, o);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (q + e < a.q.rows) row[q + e] = down<T>(a.add ? v[e] + up(row[q + e]) : v[e]);
+              for (int e = 0; e < 4; ++e) v[e] += o[e];
+            }
+            store<T, 4>(row + q, v);
+          } else if (in) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (q + e < a.q.rows) row[q + e] = down<T>(ADD ? v[e] + up(row[q + e]) : v[e]);
+          }
         }
       }
+      __builtin_amdgcn_sched_barrier(0);  // (a row's values at a time: they are many beside the sums)
     }
-  };
-  if (a.type == SIMPLE_F32) put((float*)a.out);
-  else put((uint16_t*)a.out);
   });
 }
 
@@ -484,13 +521,15 @@ int hidden_splits(int64_t T, int64_t V, int64_t D) {
   return (int)std::max<int64_t>(1, std::min(most, want / tiles));
 }
 
-struct Layout { int64_t tops, tokens, g, gt, wt, ht, sums, total, rows, t16; int splits; };
+constexpr int64_t WEIGHT_WGS = 2048;  // workgroups that look for the weights' largest magnitude
+struct Layout { int64_t tops, partial, tokens, g, gt, wt, ht, sums, total, rows, t16; int splits; };
 Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
   Layout L{};
   auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
   L.rows = piece_rows(T, V);
   L.t16 = ceil_div(T, 16) * 16;
   L.tops = take(TOPS * 4);
+  L.partial = take((ceil_div(T, 4) + WEIGHT_WGS) * 4);
   L.tokens = take(T * (int64_t)sizeof(Token));
   if (hidden) {
     L.splits = hidden_splits(T, V, D);
@@ -514,14 +553,17 @@ void transpose(const uint16_t* in, int64_t stride, int64_t rows, int64_t cols, u
     hipLaunchKernelGGL(transpose_kernel<false>, grid, dim3(256), 0, st, in, stride, rows, cols, out, out_stride, r_out, tokens, top);
 }
 
-void multiply(MulArgs a, int splits, hipStream_t st) {
+void multiply(MulArgs a, int type, bool add, int splits, hipStream_t st) {
   a.k_split = (int)(ceil_div(ceil_div(a.k_bytes, splits), KB) * KB);
-  a.vec = rows_aligned(a.out, a.stride, type_bytes(a.type), 4 * type_bytes(a.type));
+  a.vec = rows_aligned(a.out, a.stride, type_bytes(type), 16);
   // (Few steps of k, as dW of few tokens has: a tile is mostly stored, and two smaller ones on a compute unit do so in turn.)
-  shaped<F16>(a.k_bytes <= SHORT_K ? std::min<int64_t>(a.p.rows, 128) : a.p.rows, [&](auto shape) {
+  // (So too where a tile of 256 columns would be half empty.)
+  shaped<F16>(a.k_bytes <= SHORT_K || a.q.rows <= 128 ? std::min<int64_t>(a.p.rows, 128) : a.p.rows, [&](auto shape) {
     using S = decltype(shape);
     a.plan = plan<S, Cut<S>::CAN>(a.p.rows, a.q.rows, splits == 1);
-    hipLaunchKernelGGL(mul_kernel<S>, dim3((unsigned)a.plan.grid, (unsigned)splits), dim3(S::THREADS), 0, st, a);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)a.plan.grid, (unsigned)splits), dim3(S::THREADS), 0, st, a); };
+    if (type == SIMPLE_F32) { if (add) go(mul_kernel<S, float, true>); else go(mul_kernel<S, float, false>); }
+    else { if (add) go(mul_kernel<S, uint16_t, true>); else go(mul_kernel<S, uint16_t, false>); }
   });
 }
 
@@ -614,15 +656,15 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   if (dweight_dev) { a.gt = (uint16_t*)(ws + L.gt); a.gt_stride = L.t16; }
   const unsigned char* weight = (const unsigned char*)weight_dev;
   if (T > 0) {
-    hipLaunchKernelGGL(clear_kernel, dim3(1), dim3(64), 0, st, tops);
     PrepareArgs r{(const uint16_t*)hidden_dev, (const uint16_t*)weight_dev, hidden_stride, weight_stride, T, V, D, targets_dev, lse_dev, dloss_dev,
-                  logit_scale, tokens, tops, (int)ceil_div(T, 4)};
+                  logit_scale, tokens, (float*)(ws + L.partial), (int)ceil_div(T, 4)};
     // (the weights' range is dH's: its product alone reads them in 16-bit floats)
-    const dim3 grid((unsigned)(r.token_wgs + (dhidden_dev ? std::min<int64_t>(2048, ceil_div(V, 4)) : 0)));
+    const dim3 grid((unsigned)(r.token_wgs + (dhidden_dev ? std::min<int64_t>(WEIGHT_WGS, ceil_div(V, 4)) : 0)));
     if (D % 8 == 0 && rows_aligned(hidden_dev, hidden_stride, 2, 16) && rows_aligned(weight_dev, weight_stride, 2, 16))
       hipLaunchKernelGGL(prepare_kernel<8>, grid, dim3(256), 0, st, r);
     else
       hipLaunchKernelGGL(prepare_kernel<1>, grid, dim3(256), 0, st, r);
+    hipLaunchKernelGGL(tops_kernel, dim3(1), dim3(1024), 0, st, (const float*)r.partial, r.token_wgs, (int)grid.x, tops);
     if (dweight_dev)
       transpose((const uint16_t*)hidden_dev, hidden_stride, T, D, (uint16_t*)(ws + L.ht), L.t16, L.t16, tokens, tops + TOP_STATES, st);
   }
@@ -649,9 +691,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       m.out = ws + L.sums;
       m.stride = D;
       m.split_stride = T * D;
-      m.type = SIMPLE_F32;
-      m.add = v0 > 0;
-      multiply(m, L.splits, st);
+      multiply(m, SIMPLE_F32, v0 > 0, L.splits, st);
     }
     if (dweight_dev) {
       MulArgs m{};
@@ -660,10 +700,8 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       m.k_bytes = (int)(L.t16 * 2);
       m.out = (unsigned char*)dweight_dev + v0 * dweight_stride * type_bytes(dweight_dtype);
       m.stride = dweight_stride;
-      m.type = dweight_dtype;
-      m.add = accumulate != 0;
       m.top = T > 0 ? tops + TOP_STATES : nullptr;
-      multiply(m, 1, st);
+      multiply(m, dweight_dtype, accumulate != 0, 1, st);
     }
   }
   if (dhidden_dev) {

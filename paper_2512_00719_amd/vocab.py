@@ -61,28 +61,32 @@ def _dtype(t: torch.Tensor, name: str) -> int:
         raise TypeError(f"{name} is float32 or bfloat16, got {t.dtype}") from None
 
 
+# (These run ahead of every call, whose kernels may take 5 us: the usual case is one expression.)
 def _tensor(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
     """`t`, if it is a tensor of that kind on that device whose rows are dense (the last dimension's stride is 1)."""
-    if t.dtype != dtype:
+    if t.dtype is dtype and t.shape == shape and t.device == device and (t.is_contiguous() or t.stride(-1) == 1 or t.shape[-1] == 1):
+        return t
+    if t.dtype is not dtype:
         raise TypeError(f"{name} is {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, others on {device}")
-    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{name} has a stride of {t.stride(-1)} along its rows: 1 is wanted")
-    return t
+    raise ValueError(f"{name} has a stride of {t.stride(-1)} along its rows: 1 is wanted")
 
 
-def _matrix(t: torch.Tensor, name: str, dtypes=(torch.float32, torch.bfloat16)) -> torch.Tensor:
-    """A [rows, values] matrix on the current GPU, the first operand of a call."""
+def _matrix(t: torch.Tensor, name: str, dtypes=(torch.float32, torch.bfloat16)) -> torch.device:
+    """The device of a [rows, values] matrix on the current GPU, the first operand of a call."""
     if t.dim() != 2 or t.shape[1] == 0:
         raise ValueError(f"{name} is [rows, values], got shape {tuple(t.shape)}")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} is one of {dtypes}, got {t.dtype}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}: the current GPU is wanted")
-    return _tensor(t, name, t.shape, t.dtype, t.device)
+    device = t.device
+    if device.type != "cuda" or device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {device}: the current GPU is wanted")
+    if not t.is_contiguous():
+        _tensor(t, name, t.shape, t.dtype, device)
+    return device
 
 
 def _stride(t: Optional[torch.Tensor]) -> int:
@@ -98,6 +102,10 @@ def _ptr(t: Optional[torch.Tensor]) -> int:
 
 def _out(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
     return torch.empty(shape, dtype=dtype, device=device) if t is None else _tensor(t, name, shape, dtype, device)
+
+
+def _like(t: Optional[torch.Tensor], name: str, other: torch.Tensor) -> torch.Tensor:
+    return torch.empty(other.shape, dtype=other.dtype, device=other.device) if t is None else _tensor(t, name, other.shape, other.dtype, other.device)
 
 
 def _workspace(nbytes: int, where: str, device: torch.device) -> torch.Tensor:
