@@ -108,19 +108,42 @@ template <bool DIRECT> void launch_for(const Args& a, hipStream_t st) {
 
 using namespace simple::head;
 
+extern "C" int64_t simple_linear_int8_workspace(int64_t T, int64_t V, int64_t K) {
+  if (T < 0 || V <= 0 || K <= 0) return SIMPLE_EINVAL;
+  return T <= FEW_TOKENS ? 0 : (T + (V < ALIGN_ROWS ? V : ALIGN_ROWS)) * aligned_stride(K);
+}
+
 extern "C" int simple_linear_int8(const int8_t* codes_dev, int64_t code_stride, const float* scales_dev, const int8_t* w_codes_dev,
                                   int64_t w_code_stride, const float* w_scales_dev, int64_t T, int64_t V, int64_t K, void* out_dev,
-                                  int64_t out_stride, int out_dtype, void* hip_stream) {
+                                  int64_t out_stride, int out_dtype, void* workspace_dev, int64_t workspace_bytes, void* hip_stream) {
   if (T < 0 || V <= 0 || K <= 0 || code_stride < K || w_code_stride < K || out_stride < V || !good_type(out_dtype)) return SIMPLE_EINVAL;
   if (K > MAX_K || T > ((int64_t)1 << 24) || V > ((int64_t)1 << 28)) return SIMPLE_ECAPACITY;
   if (T == 0) return SIMPLE_OK;
   if (!codes_dev || !scales_dev || !w_codes_dev || !w_scales_dev || !out_dev) return SIMPLE_EINVAL;
+  if (workspace_dev && ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
+  if (workspace_dev && workspace_bytes < simple_linear_int8_workspace(T, V, K)) return SIMPLE_ECAPACITY;
   if (ceil_div(T, 16) * ceil_div(V, 64) > (int64_t)0x7FFFFFFF) return SIMPLE_ECAPACITY;
   const int64_t e = type_bytes(out_dtype);
   Args a{{(const unsigned char*)codes_dev, code_stride, T}, {(const unsigned char*)w_codes_dev, w_code_stride, V}, (int)K, out_dtype, Plan{},
          rows_aligned(out_dev, out_stride, e, 16), scales_dev, w_scales_dev, out_dev, out_stride};
   hipStream_t st = (hipStream_t)hip_stream;
-  if (direct(a.tokens, K) && direct(a.weights, K)) launch_for<true>(a, st);
-  else launch_for<false>(a, st);
+  const Operand weights = a.weights;
+  const bool tokens_fit = direct(a.tokens, K), weights_fit = direct(weights, K);
+  if (tokens_fit && weights_fit) {
+    launch_for<true>(a, st);
+  } else if (T <= FEW_TOKENS || !workspace_dev) {
+    launch_for<false>(a, st);
+  } else {  // copies with aligned rows, of the weights ALIGN_ROWS at a time
+    unsigned char* ws = (unsigned char*)workspace_dev;
+    const int64_t stride = aligned_stride(K);
+    a.k_bytes = (int)stride;
+    a.tokens = aligned_copy<1>(a.tokens, K, ws, st);
+    for (int64_t v0 = 0; v0 < V; v0 += ALIGN_ROWS) {
+      a.weights = aligned_copy<1>(Operand{weights.p + v0 * weights.stride, weights.stride, V - v0 < ALIGN_ROWS ? V - v0 : ALIGN_ROWS}, K, ws + T * stride, st);
+      a.w_scales = w_scales_dev + v0;
+      a.out = (unsigned char*)out_dev + v0 * e;
+      launch_for<true>(a, st);
+    }
+  }
   return launched();
 }

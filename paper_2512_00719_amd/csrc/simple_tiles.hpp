@@ -128,24 +128,24 @@ template <class S, bool MANY> inline Plan plan(int64_t p_rows, int64_t q_rows, b
   return r;
 }
 
-// 16 bytes of a row from byte `k` on, zeros behind its end; any alignment.
-template <int BYTES> __device__ __forceinline__ i32x4 chunk_of(const unsigned char* row, int64_t k, int64_t k_bytes) {
-  i32x4 v = {0, 0, 0, 0};
-  if (k + 16 <= k_bytes) {
-    __builtin_memcpy(&v, row + k, 16);
-  } else if (k < k_bytes) {
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
+// 16 bytes of a row from byte `k` on, zeros behind its end; any alignment.  A row's last bytes come from the 16 that end with it.  In two parts, so
+// that what is loaded is not looked at before it is wanted: taken_from() makes of the loaded what it stands for.
+typedef unsigned __int128 u128;
+template <int BYTES> __device__ __forceinline__ u128 chunk_at(const unsigned char* row, int k, int k_bytes) {
+  u128 v = 0;
+  if (k_bytes >= 16) {
+    __builtin_memcpy(&v, row + min(k, k_bytes - 16), 16);
+  } else if (k == 0) {
 #pragma unroll
-    for (int i = 0; i < 16 / BYTES; ++i) {
-      const int at = i * BYTES;
-      if (k + at < k_bytes) {
-        const uint32_t e = BYTES == 1 ? (uint32_t)row[k + at] : (uint32_t)*reinterpret_cast<const uint16_t*>(row + k + at);
-        w[at / 4] |= e << (8 * (at % 4));
-      }
-    }
-    v = i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+    for (int i = 0; i < 16; i += BYTES)
+      if (i < k_bytes) v |= (u128)(BYTES == 1 ? (uint32_t)row[i] : (uint32_t)*reinterpret_cast<const uint16_t*>(row + i)) << (8 * i);
   }
   return v;
+}
+__device__ __forceinline__ i32x4 taken_from(u128 v, int k, int k_bytes) {
+  const int over = k + 16 - max(k_bytes, 16);  // bytes of the chunk behind the row's end
+  if (over > 0) v = over < 16 ? v >> (8 * over) : 0;
+  return __builtin_bit_cast(i32x4, v);
 }
 
 // Rows of a tile on their way to LDS by to_lds().  Rows behind an operand's last repeat it (what they give is not stored).
@@ -327,31 +327,41 @@ __device__ __forceinline__ void products(const Operand& P, const Operand& Q, int
       for (int i = 0; i < S::LP; ++i) row_p[i] = P.p + (p0 + min((wave + i * S::NW) % S::GP * 8 + row8, p_rows - 1)) * P.stride;
 #pragma unroll
       for (int i = 0; i < S::LQ; ++i) row_q[i] = Q.p + (q0 + min((wave + i * S::NW) % S::GQ * 8 + row8, q_rows - 1)) * Q.stride;
-      i32x4 v[S::LP + S::LQ];
-      auto fetch = [&](int s) {
-        const int64_t k = (int64_t)s * KB + chunk * 16;
+      // AHEAD steps in registers: as many in flight as the direct stages have where the memory is what bounds
+      constexpr int AHEAD = S::STAGES > 2 ? S::STAGES - 1 : S::BP * S::BQ <= 128 * 128 ? 2 : 1, NL = S::LP + S::LQ;
+      u128 v[AHEAD][NL];
+      auto fetch = [&](int s, u128 (&x)[NL]) {
+        const int k = s * KB + chunk * 16;
 #pragma unroll
-        for (int i = 0; i < S::LP; ++i) v[i] = chunk_of<S::E::BYTES>(row_p[i], k, k_bytes);
+        for (int i = 0; i < S::LP; ++i) x[i] = chunk_at<S::E::BYTES>(row_p[i], k, k_bytes);
 #pragma unroll
-        for (int i = 0; i < S::LQ; ++i) v[S::LP + i] = chunk_of<S::E::BYTES>(row_q[i], k, k_bytes);
+        for (int i = 0; i < S::LQ; ++i) x[S::LP + i] = chunk_at<S::E::BYTES>(row_q[i], k, k_bytes);
       };
-      auto put = [&](int stage) {
-        unsigned char* b = lds + stage * S::STAGE + lane * 16;
+      auto put = [&](int s, const u128 (&x)[NL]) {
+        const int k = s * KB + chunk * 16;
+        unsigned char* b = lds + (s & 1) * S::STAGE + lane * 16;
 #pragma unroll
-        for (int i = 0; i < S::LP; ++i) *reinterpret_cast<i32x4*>(b + (wave + i * S::NW) % S::GP * 1024) = v[i];
+        for (int i = 0; i < S::LP; ++i) *reinterpret_cast<i32x4*>(b + (wave + i * S::NW) % S::GP * 1024) = taken_from(x[i], k, k_bytes);
 #pragma unroll
-        for (int i = 0; i < S::LQ; ++i) *reinterpret_cast<i32x4*>(b + S::BP * KB + (wave + i * S::NW) % S::GQ * 1024) = v[S::LP + i];
+        for (int i = 0; i < S::LQ; ++i) *reinterpret_cast<i32x4*>(b + S::BP * KB + (wave + i * S::NW) % S::GQ * 1024) = taken_from(x[S::LP + i], k, k_bytes);
       };
       clear();
-      fetch(0);
-      __syncthreads();  // the tile before is read
-      put(0);
-      for (int s = 0; s < steps; ++s) {
-        __syncthreads();
-        if (s + 1 < steps) fetch(s + 1);
-        step(s & 1);
-        if (s + 1 < steps) put((s + 1) & 1);  // read last in the step before, ahead of the barrier
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (u < steps) fetch(u, v[u]);
+      for (int s0 = 0; s0 < steps; s0 += AHEAD) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          const int s = s0 + u;
+          if (s < steps) {
+            put(s, v[u]);  // read last two steps ago, ahead of the barrier of the step before
+            if (s + AHEAD < steps) fetch(s + AHEAD, v[u]);
+            __syncthreads();
+            step(s & 1);
+          }
+        }
       }
+      __syncthreads();  // (the next tile's first step, or done())
       done(acc, p0, q0);
       if constexpr (!MANY) break;
     }
@@ -384,6 +394,33 @@ __device__ __forceinline__ void planned(const Operand& P, const Operand& Q, int 
     q0 = (int64_t)q * S::BQ;
     return true;
   }, [&](auto& acc, int64_t p0, int64_t q0) { done(S{}, acc, p0, q0); });
+}
+
+// Rows of any alignment, copied to rows of `out_stride` bytes (a multiple of 16), zeros behind their end.  Many tokens read a weight
+// row often: with rows that start anywhere staged through registers, 2000 tokens x 50,001 x 1023 bfloat16 took 514 us, and 204 + 45 for
+// the copy so; up to FEW_TOKENS the copy costs what it saves.
+constexpr int64_t FEW_TOKENS = 128;
+constexpr int64_t ALIGN_ROWS = 65536;  // weights at a time
+template <int BYTES> __global__ __launch_bounds__(256) void align_kernel(const unsigned char* in, int64_t stride, int64_t rows, int64_t bytes, unsigned char* out,
+                                                                         int64_t out_stride) {
+  const int64_t chunks = out_stride / 16, c = (int64_t)blockIdx.y * blockDim.x + threadIdx.x;
+  if (c >= chunks) return;
+  const int64_t r0 = (int64_t)blockIdx.x * (blockDim.y * 4) + threadIdx.y;
+  u128 v[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = chunk_at<BYTES>(in + min(r0 + k * blockDim.y, rows - 1) * stride, (int)c * 16, (int)bytes);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (r0 + k * blockDim.y < rows) *reinterpret_cast<i32x4*>(out + (r0 + k * blockDim.y) * out_stride + c * 16) = taken_from(v[k], (int)c * 16, (int)bytes);
+}
+inline int64_t aligned_stride(int64_t k_bytes) { return ceil_div(k_bytes, 16) * 16; }
+template <int BYTES> inline Operand aligned_copy(const Operand& o, int64_t k_bytes, unsigned char* to, hipStream_t st) {
+  const int64_t stride = aligned_stride(k_bytes), chunks = stride / 16;
+  int x = 8;
+  while (x < 256 && x < chunks) x *= 2;
+  hipLaunchKernelGGL((align_kernel<BYTES>), dim3((unsigned)ceil_div(o.rows, 256 / x * 4), (unsigned)ceil_div(chunks, x)), dim3(x, 256 / x), 0, st, o.p, o.stride,
+                     o.rows, k_bytes, to, stride);
+  return Operand{to, stride, o.rows};
 }
 
 // Whether products<S, true> takes the operand: its resource's offsets stay below 2^31.

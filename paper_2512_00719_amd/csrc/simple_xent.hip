@@ -15,6 +15,7 @@
 // Tokens whose target is outside the vocabulary or whose dl is 0 take no part: their states are read as zeros where sums over tokens are
 // formed, so that a NaN in them stays with them.
 #include <algorithm>
+#include <type_traits>
 
 #include "simple_tiles.hpp"
 
@@ -40,7 +41,7 @@ struct Args {
   const int32_t* targets;
   int64_t V, v0;           // whole vocabulary, the piece's first row
   // forward
-  Pair* pairs;             // [nq][T]
+  Pair* pairs;             // [tiles of the piece][T]
   float* at_target;        // [T]
   // gradient
   const struct Token* tokens;
@@ -54,8 +55,8 @@ __device__ __forceinline__ void stats_of(const Args& a, typename S::Acc (&acc)[S
   const int64_t T = a.hidden.rows;
   const int lane = opaque_lane(), wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
   const int64_t q1 = q0 + wq * S::FQ * 16 + (lane >> 4) * 4;
-  const int left = (int)min((int64_t)S::BQ, a.V - q1);  // the lane's columns that exist
-  if (q0 + S::BQ > a.V) {
+  const int left = (int)min((int64_t)S::BQ, a.weight.rows - q1);  // the lane's columns that exist
+  if (q0 + S::BQ > a.weight.rows) {
 #pragma unroll
     for (int i = 0; i < S::FQ; ++i)
 #pragma unroll
@@ -71,7 +72,7 @@ __device__ __forceinline__ void stats_of(const Args& a, typename S::Acc (&acc)[S
   for (int j = 0; j < S::FP; ++j) {
     const int pl = (wp * S::FP + j) * 16 + (lane & 15);
     const int64_t p = p0 + pl;
-    const int64_t target = p < T ? (int64_t)a.targets[p] - q1 : -1;
+    const int64_t target = p < T ? (int64_t)a.targets[p] - a.v0 - q1 : -1;
     if (target >= 0 && target < S::FQ * 16 && target < left) {  // (few tiles hold a token's target)
 #pragma unroll
       for (int i = 0; i < S::FQ; ++i)
@@ -227,25 +228,34 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
   constexpr int AHEAD = 8;  // loads in flight
   float top = 0.f;
   const int64_t waves = ((int64_t)gridDim.x - a.token_wgs) * 4;
-  const bool whole = a.weight_stride == a.D;  // one long row, taken in pieces of what a wave has in flight
-  constexpr int64_t PIECE = 64 * VEC * AHEAD;
-  const int64_t n = whole ? ceil_div(a.V * a.D, PIECE) : a.V;
-  for (int64_t v = ((int64_t)blockIdx.x - a.token_wgs) * 4 + wave; v < n; v += waves) {
-    const uint16_t* w = a.weight + (whole ? v * PIECE : v * a.weight_stride);
-    const int64_t end = whole ? min(PIECE, a.V * a.D - v * PIECE) : a.D;
-    for (int64_t c = lane * VEC; c < end; c += PIECE) {
-      float x[AHEAD][VEC];
+  const int64_t first = ((int64_t)blockIdx.x - a.token_wgs) * 4 + wave;
+  // `n` rows of `len` values in groups of W, a wave's loads of a row in flight together
+  auto look = [&](auto width, const uint16_t* w, int64_t stride, int64_t n, int64_t len) {
+    constexpr int W = decltype(width)::value;
+    for (int64_t v = first; v < n; v += waves)
+      for (int64_t c = lane * W; c < len; c += 64 * W * AHEAD) {
+        float x[AHEAD][W];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x[u][e] = 0.f;
-        if (c + u * 64 * VEC < end) load<uint16_t, VEC>(w + c + u * 64 * VEC, x[u]);
+          for (int e = 0; e < W; ++e) x[u][e] = 0.f;
+          if (c + u * 64 * W < len) load<uint16_t, W>(w + v * stride + c + u * 64 * W, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+          for (int e = 0; e < W; ++e) top = larger(top, x[u][e]);
       }
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) top = larger(top, x[u][e]);
+  };
+  const int64_t all = a.V * a.D;
+  if (a.weight_stride == a.D && ((uintptr_t)a.weight & 15u) == 0) {  // one long row, whatever D is: rows of a wave's loads, then what is left
+    constexpr int64_t LONG = 64 * 8 * AHEAD;
+    look(std::integral_constant<int, 8>{}, a.weight, LONG, all / LONG, LONG);
+    if (first == 0) {
+      for (int64_t c = all / LONG * LONG + lane; c < all; c += 64) top = larger(top, up(a.weight[c]));
     }
+  } else {
+    look(std::integral_constant<int, VEC>{}, a.weight, a.weight_stride, a.V, a.D);
   }
   top = top_of<4>(top, part);
   if (threadIdx.x == 0) a.partial[blockIdx.x] = top;
@@ -522,12 +532,16 @@ int hidden_splits(int64_t T, int64_t V, int64_t D) {
 }
 
 constexpr int64_t WEIGHT_WGS = 2048;  // workgroups that look for the weights' largest magnitude
-struct Layout { int64_t tops, partial, tokens, g, gt, wt, ht, sums, total, rows, t16; int splits; };
+struct Layout { int64_t copy_h, copy_w, tops, partial, tokens, g, gt, wt, ht, sums, total, rows, t16; int splits; };
 Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
   Layout L{};
   auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
   L.rows = piece_rows(T, V);
   L.t16 = ceil_div(T, 16) * 16;
+  if (T > FEW_TOKENS) {  // (for rows that are not aligned)
+    L.copy_h = take(T * aligned_stride(D * 2));
+    L.copy_w = take(L.rows * aligned_stride(D * 2));
+  }
   L.tops = take(TOPS * 4);
   L.partial = take((ceil_div(T, 4) + WEIGHT_WGS) * 4);
   L.tokens = take(T * (int64_t)sizeof(Token));
@@ -585,7 +599,9 @@ int64_t pairs_bytes(int64_t T, int64_t V) { return ((ceil_div(V, tile_q(T)) * T 
 
 extern "C" int64_t simple_xent_workspace(int64_t T, int64_t V, int64_t D) {
   const int rc = check_sizes(T, V, D);
-  return rc != SIMPLE_OK ? rc : pairs_bytes(T, V) + T * 4;
+  if (rc != SIMPLE_OK) return rc;
+  const int64_t copies = T > FEW_TOKENS ? (T + std::min(V, ALIGN_ROWS)) * aligned_stride(D * 2) : 0;
+  return pairs_bytes(T, V) + ((T * 4 + 255) & ~(int64_t)255) + copies;
 }
 
 extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, const int32_t* targets_dev,
@@ -599,24 +615,40 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
   if (!workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
   if (workspace_bytes < simple_xent_workspace(T, V, D)) return SIMPLE_ECAPACITY;
   hipStream_t st = (hipStream_t)hip_stream;
+  unsigned char* ws = (unsigned char*)workspace_dev;
   Args a{};
   a.hidden = {(const unsigned char*)hidden_dev, hidden_stride * 2, T};
-  a.weight = {(const unsigned char*)weight_dev, weight_stride * 2, V};
+  const Operand weight{(const unsigned char*)weight_dev, weight_stride * 2, V};
   a.k_bytes = (int)(D * 2);
   a.scale = logit_scale;
   a.targets = targets_dev;
   a.V = V;
-  a.pairs = (Pair*)workspace_dev;
-  a.at_target = (float*)((unsigned char*)workspace_dev + pairs_bytes(T, V));
-  const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
-  shaped<Bf16>(T, [&](auto shape) {
-    using S = decltype(shape);
-    a.plan = plan<S, false>(T, V);
-    const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
-    if (dir) hipLaunchKernelGGL((stats_kernel<S, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((stats_kernel<S, false>), grid, block, 0, st, a);
-  });
-  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)ceil_div(T, FIN_T)), dim3(FIN_T * FIN_GROUPS), 0, st, (const Pair*)a.pairs, a.plan.nq, T, V, targets_dev,
+  a.at_target = (float*)(ws + pairs_bytes(T, V));
+  const int64_t tiles_q = ceil_div(V, tile_q(T));
+  auto stats = [&](const Operand& w, int64_t v0, bool dir) {
+    a.weight = w;
+    a.v0 = v0;
+    a.pairs = (Pair*)ws + v0 / tile_q(T) * T;
+    shaped<Bf16>(T, [&](auto shape) {
+      using S = decltype(shape);
+      a.plan = plan<S, false>(T, w.rows);
+      const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
+      if (dir) hipLaunchKernelGGL((stats_kernel<S, true>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((stats_kernel<S, false>), grid, block, 0, st, a);
+    });
+  };
+  if (direct(a.hidden, a.k_bytes) && direct(weight, a.k_bytes)) {
+    stats(weight, 0, true);
+  } else if (T <= FEW_TOKENS) {
+    stats(weight, 0, false);
+  } else {  // copies with aligned rows, of the weights ALIGN_ROWS (a multiple of every tile) at a time
+    unsigned char* room = ws + pairs_bytes(T, V) + ((T * 4 + 255) & ~(int64_t)255);
+    a.hidden = aligned_copy<2>(a.hidden, D * 2, room, st);
+    a.k_bytes = (int)a.hidden.stride;
+    for (int64_t v0 = 0; v0 < V; v0 += ALIGN_ROWS)
+      stats(aligned_copy<2>(Operand{weight.p + v0 * weight.stride, weight.stride, std::min(ALIGN_ROWS, V - v0)}, D * 2, room + T * a.hidden.stride, st), v0, true);
+  }
+  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)ceil_div(T, FIN_T)), dim3(FIN_T * FIN_GROUPS), 0, st, (const Pair*)ws, (int)tiles_q, T, V, targets_dev,
                      (const float*)a.at_target, loss_dev, lse_dev);
   return launched();
 }
@@ -668,10 +700,16 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
     if (dweight_dev)
       transpose((const uint16_t*)hidden_dev, hidden_stride, T, D, (uint16_t*)(ws + L.ht), L.t16, L.t16, tokens, tops + TOP_STATES, st);
   }
+  const bool copies = T > FEW_TOKENS && !(direct(a.hidden, D * 2) && direct(Operand{weight, weight_stride * 2, V}, D * 2));
+  if (copies) {
+    a.hidden = aligned_copy<2>(a.hidden, D * 2, ws + L.copy_h, st);
+    a.k_bytes = (int)a.hidden.stride;
+  }
   for (int64_t v0 = 0; v0 < V; v0 += L.rows) {
     const int64_t n = std::min(L.rows, V - v0), n8 = ceil_div(n, 8) * 8;
     a.weight = {weight + v0 * weight_stride * 2, weight_stride * 2, n};
     a.v0 = v0;
+    if (copies) a.weight = aligned_copy<2>(a.weight, D * 2, ws + L.copy_w, st);
     if (T > 0) {
       const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
       shaped<Bf16>(T, [&](auto shape) {
@@ -683,7 +721,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       });
     }
     if (dhidden_dev) {
-      transpose((const uint16_t*)a.weight.p, weight_stride, n, D, (uint16_t*)(ws + L.wt), L.rows, n8, nullptr, tops + TOP_WEIGHTS, st);
+      transpose((const uint16_t*)a.weight.p, a.weight.stride / 2, n, D, (uint16_t*)(ws + L.wt), L.rows, n8, nullptr, tops + TOP_WEIGHTS, st);
       MulArgs m{};
       m.p = {(const unsigned char*)a.g, a.g_stride * 2, T};
       m.q = {ws + L.wt, L.rows * 2, D};

@@ -17,7 +17,7 @@ from . import binding
 from .binding import SIMPLE_BF16, SIMPLE_F32, SIMPLE_OK, SimpleError, _addresses, _current_stream
 
 EXPORTS = ("simple_rms_norm", "simple_rms_norm_int8", "simple_quantize_rows", "simple_rms_norm_grad", "simple_rms_norm_grad_workspace",
-           "simple_embed", "simple_embed_grad", "simple_embed_grad_workspace", "simple_linear_int8",
+           "simple_embed", "simple_embed_grad", "simple_embed_grad_workspace", "simple_linear_int8", "simple_linear_int8_workspace",
            "simple_xent", "simple_xent_workspace", "simple_xent_grad", "simple_xent_grad_workspace")
 
 
@@ -32,7 +32,8 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
         "simple_embed": (ci, vp, vp, i64, i64, i64, i64, ci, f32, vp, i64, vp),
         "simple_embed_grad": (ci, vp, vp, i64, i64, i64, i64, ci, f32, vp, i64, ci, ci, vp, i64, vp),
         "simple_embed_grad_workspace": (i64, i64, i64, i64),
-        "simple_linear_int8": (ci, vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, i64, ci, vp),
+        "simple_linear_int8": (ci, vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, i64, ci, vp, i64, vp),
+        "simple_linear_int8_workspace": (i64, i64, i64, i64),
         "simple_xent": (ci, vp, i64, vp, i64, vp, i64, i64, i64, f32, vp, vp, vp, i64, vp),
         "simple_xent_workspace": (i64, i64, i64, i64),
         "simple_xent_grad": (ci, vp, vp, i64, vp, i64, vp, vp, i64, i64, i64, f32, vp, i64, vp, i64, ci, ci, vp, i64, vp),
@@ -225,8 +226,11 @@ def linear_int8(codes, scales, w_codes, w_scales, *, out_dtype: torch.dtype = to
     if out_dtype not in _TYPES:
         raise TypeError(f"logits are float32 or bfloat16, got {out_dtype}")
     out = _out(out, "out", (T, V), out_dtype, codes.device)
+    rows = codes.data_ptr() | w_codes.data_ptr() | _stride(codes) | _stride(w_codes) | K
+    ws = _workspace(_lib.simple_linear_int8_workspace(T, V, K), "simple_linear_int8_workspace", codes.device) if T > 128 and rows % 16 else None
     _check(_lib.simple_linear_int8(codes.data_ptr(), _stride(codes), scales.data_ptr(), w_codes.data_ptr(), _stride(w_codes), w_scales.data_ptr(),
-                                   T, V, K, out.data_ptr(), _stride(out), _TYPES[out_dtype], _current_stream()), "simple_linear_int8")
+                                   T, V, K, out.data_ptr(), _stride(out), _TYPES[out_dtype], _ptr(ws), 0 if ws is None else ws.numel(),
+                                   _current_stream()), "simple_linear_int8")
     return out
 
 
