@@ -55,7 +55,7 @@ template <int NT> __device__ __forceinline__ void row_reduce(float& sum, uint32_
 }
 
 // NT threads a row, NV groups of VEC values a thread.
-template <typename T, int VEC, int NT, int NV, int OUT>
+template <typename T, int VEC, bool WHOLE, int NT, int NV, int OUT>
 __global__ __launch_bounds__(NT > WG ? NT : WG) void rows_kernel(Args a) {
   constexpr int ROWS = NT > WG ? 1 : WG / NT;
   __shared__ float part[2 * (NT > 64 ? NT / 64 : 1)];
@@ -68,8 +68,8 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void rows_kernel(Args a) {
   for (int i = 0; i < NV; ++i) {
     const int c = (i * NT + t) * VEC;
     if (c < a.D) {
-      load<T, VEC>(x + c, h[i]);
-      if constexpr (OUT != QUANT) load<T, VEC>((const T*)a.weight + c, w[i]);
+      load_some<T, VEC, WHOLE>(x, c, a.D, h[i]);
+      if constexpr (OUT != QUANT) load_some<T, VEC, WHOLE>((const T*)a.weight, c, a.D, w[i]);
     }
   }
   if (OUT != QUANT && a.residual) {
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void rows_kernel(Args a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * NT + t) * VEC;
-      if (c < a.D) load<T, VEC>(r + c, e[i]);
+      if (c < a.D) load_some<T, VEC, WHOLE>(r, c, a.D, e[i]);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i)  // the norm is of the stream as it is kept, so that its gradient finds the same values
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void rows_kernel(Args a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * NT + t) * VEC;
-      if (c < a.D) store<T, VEC>(ho + c, h[i]);
+      if (c < a.D) store_some<T, VEC, WHOLE>(ho + c, a.D - c, h[i]);
     }
   }
   if (OUT != QUANT && a.rstd && t == 0) a.rstd[row] = s;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void rows_kernel(Args a) {
         float y[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) y[j] = h[i][j] * s * w[i][j];
-        store<T, VEC>(o + c, y);
+        store_some<T, VEC, WHOLE>(o + c, a.D - c, y);
       }
     }
   } else {
@@ -133,10 +133,10 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void rows_kernel(Args a) {
     for (int i = 0; i < NV; ++i) {
       const int c = (i * NT + t) * VEC;
       if (c < a.D) {
-        Group<int8_t, VEC> q;
+        int8_t q[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) q.v[j] = (bad || none) ? (int8_t)0 : (int8_t)(int)rintf(w[i][j] * r);
-        *reinterpret_cast<Group<int8_t, VEC>*>(o + c) = q;
+        for (int j = 0; j < VEC; ++j) q[j] = (bad || none) ? (int8_t)0 : (int8_t)(int)rintf(w[i][j] * r);
+        put_some<int8_t, VEC, WHOLE>(o + c, a.D - c, q);
       }
     }
   }
@@ -153,7 +153,7 @@ struct GradArgs {
 
 // A workgroup takes rows a grid apart, so that each of its threads adds up the same columns' weight gradient in registers over all of
 // them; the workgroups' sums are joined by column_sums_kernel in their order.
-template <typename T, int VEC, int NT, int NV>
+template <typename T, int VEC, bool WHOLE, int NT, int NV>
 __global__ __launch_bounds__(NT > WG ? NT : WG) void grad_kernel(GradArgs a) {
   constexpr int ROWS = NT > WG ? 1 : WG / NT;
   __shared__ float part[2][2 * (NT > 64 ? NT / 64 : 1)];
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void grad_kernel(GradArgs a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (i * NT + t) * VEC;
-    if (c < a.D) load<T, VEC>((const T*)a.weight + c, w[i]);
+    if (c < a.D) load_some<T, VEC, WHOLE>((const T*)a.weight, c, a.D, w[i]);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) dw[i][j] = 0.f;
   }
@@ -176,9 +176,9 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void grad_kernel(GradArgs a) {
     for (int i = 0; i < NV; ++i) {
       const int c = (i * NT + t) * VEC;
       if (c < a.D) {
-        load<T, VEC>(dy + c, g[i]);
-        load<T, VEC>(h + c, n[i]);
-        if (a.dh) load<T, VEC>((const T*)a.dh + row * a.dh_stride + c, e[i]);
+        load_some<T, VEC, WHOLE>(dy, c, a.D, g[i]);
+        load_some<T, VEC, WHOLE>(h, c, a.D, n[i]);
+        if (a.dh) load_some<T, VEC, WHOLE>((const T*)a.dh + row * a.dh_stride, c, a.D, e[i]);
       }
     }
     float sum = 0.f;
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void grad_kernel(GradArgs a) {
           g[i][j] = s * (g[i][j] - n[i][j] * m);
           if (a.dh) g[i][j] += e[i][j];
         }
-        store<T, VEC>(dx + c, g[i]);
+        store_some<T, VEC, WHOLE>(dx + c, a.D - c, g[i]);
       }
     }
   }
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void grad_kernel(GradArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * NT + t) * VEC;
-      if (c < a.D) store<float, VEC>(out + c, dw[i]);  // (D is a multiple of VEC)
+      if (c < a.D) store_some<float, VEC, WHOLE>(out + c, a.D - c, dw[i]);
     }
   }
 }
@@ -266,16 +266,17 @@ template <typename F> void shaped(int64_t D, F&& f) {
   else if (D <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 32>{});
   else f(integral_constant<int, 1024>{}, integral_constant<int, 32>{});
 }
-// Elements a load: 16 bytes where all rows allow it, 4 bytes, or one.
-template <typename F> void typed(int dtype, int64_t align, F&& f) {
+// 16 bytes a load.  Rows that are not aligned, or end inside one: bfloat16 takes unaligned loads (8192 rows of 2047 values: norm 32 us and its gradient 38, 40 and 58
+// by single elements; aligned rows of 2048 24 and 28), float32 single elements (46 and 56 us, 57 and 64 by unaligned loads; aligned 42 and 52).
+template <typename F> void typed(int dtype, bool whole, F&& f) {
+  using std::bool_constant;
   using std::integral_constant;
   if (dtype == SIMPLE_F32) {
-    if (align == 16) f((float*)nullptr, integral_constant<int, 4>{});
-    else f((float*)nullptr, integral_constant<int, 1>{});
+    if (whole) f((float*)nullptr, integral_constant<int, 4>{}, bool_constant<true>{});
+    else f((float*)nullptr, integral_constant<int, 1>{}, bool_constant<true>{});
   } else {
-    if (align == 16) f((uint16_t*)nullptr, integral_constant<int, 8>{});
-    else if (align == 4) f((uint16_t*)nullptr, integral_constant<int, 2>{});
-    else f((uint16_t*)nullptr, integral_constant<int, 1>{});
+    if (whole) f((uint16_t*)nullptr, integral_constant<int, 8>{}, bool_constant<true>{});
+    else f((uint16_t*)nullptr, integral_constant<int, 8>{}, bool_constant<false>{});
   }
 }
 
@@ -283,19 +284,16 @@ bool bad_rows(const void* p, int64_t stride, int64_t D) { return p == nullptr ||
 
 template <int OUT> int launch_rows(const Args& a, int dtype, hipStream_t st) {
   const int64_t e = type_bytes(dtype);
-  auto all = [&](int64_t to) {  // codes of a group are stored together too
-    const int64_t vec = to / e;
-    return (a.D % vec) == 0 && rows_aligned(a.x, a.x_stride, e, to) && rows_aligned(a.residual, a.residual_stride, e, to) &&
-           rows_aligned(a.weight, 0, e, to) && rows_aligned(a.h, a.h_stride, e, to) &&
-           (OUT == NORM ? rows_aligned(a.out, a.out_stride, e, to) : rows_aligned(a.out, a.out_stride, 1, vec));
-  };
-  const int64_t align = all(16) ? 16 : all(4) ? 4 : e;
-  typed(dtype, align, [&](auto* type, auto vec) {
+  const int64_t vec = 16 / e;
+  const bool whole = a.D % vec == 0 && rows_aligned(a.x, a.x_stride, e, 16) && rows_aligned(a.residual, a.residual_stride, e, 16) &&
+                     rows_aligned(a.weight, 0, e, 16) && rows_aligned(a.h, a.h_stride, e, 16) &&
+                     (OUT == NORM ? rows_aligned(a.out, a.out_stride, e, 16) : rows_aligned(a.out, a.out_stride, 1, vec));
+  typed(dtype, whole, [&](auto* type, auto vec, auto aligned) {
     shaped(a.D, [&](auto nt, auto ept) {
       using T = std::remove_pointer_t<decltype(type)>;
       constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value, NV = decltype(ept)::value / VEC;
       constexpr int ROWS = NT > WG ? 1 : WG / NT;
-      hipLaunchKernelGGL((rows_kernel<T, VEC, NT, NV, OUT>), dim3((unsigned)ceil_div(a.T, ROWS)), dim3(NT > WG ? NT : WG), 0, st, a);
+      hipLaunchKernelGGL((rows_kernel<T, VEC, decltype(aligned)::value, NT, NV, OUT>), dim3((unsigned)ceil_div(a.T, ROWS)), dim3(NT > WG ? NT : WG), 0, st, a);
     });
   });
   return launched();
@@ -377,15 +375,13 @@ extern "C" int simple_rms_norm_grad(const void* dy_dev, int64_t dy_stride, const
     if (workspace_bytes < simple_rms_norm_grad_workspace(T, D)) return SIMPLE_ECAPACITY;
     const GradArgs a{dy_dev, h_dev, weight_dev, dh_dev, rstd_dev, dy_stride, h_stride, dh_stride, dx_stride, T, (int)D, dx_dev, (float*)workspace_dev};
     const int64_t e = type_bytes(dtype);
-    auto all = [&](int64_t to) {
-      return (D % (to / e)) == 0 && rows_aligned(dy_dev, dy_stride, e, to) && rows_aligned(h_dev, h_stride, e, to) &&
-             rows_aligned(weight_dev, 0, e, to) && rows_aligned(dh_dev, dh_stride, e, to) && rows_aligned(dx_dev, dx_stride, e, to);
-    };
-    typed(dtype, all(16) ? 16 : all(4) ? 4 : e, [&](auto* type, auto vec) {
+    const bool whole = D % (16 / e) == 0 && rows_aligned(dy_dev, dy_stride, e, 16) && rows_aligned(h_dev, h_stride, e, 16) &&
+                       rows_aligned(weight_dev, 0, e, 16) && rows_aligned(dh_dev, dh_stride, e, 16) && rows_aligned(dx_dev, dx_stride, e, 16);
+    typed(dtype, whole, [&](auto* type, auto vec, auto aligned) {
       shaped(D, [&](auto nt, auto ept) {
         using E = std::remove_pointer_t<decltype(type)>;
         constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value, NV = decltype(ept)::value / VEC;
-        hipLaunchKernelGGL((grad_kernel<E, VEC, NT, NV>), dim3((unsigned)grad_workgroups(T, D)), dim3(NT > WG ? NT : WG), 0, st, a);
+        hipLaunchKernelGGL((grad_kernel<E, VEC, decltype(aligned)::value, NT, NV>), dim3((unsigned)grad_workgroups(T, D)), dim3(NT > WG ? NT : WG), 0, st, a);
       });
     });
   }

@@ -36,6 +36,55 @@ template <typename T, int VEC> __device__ __forceinline__ void store(T* p, const
   *reinterpret_cast<Group<T, VEC>*>(p) = g;
 }
 
+// VEC elements of a row of `len` from its element c < len on, zeros behind its end.  WHOLE: rows are aligned and c + VEC is in the row; else any
+// alignment (an access of 16 bytes may start anywhere): a row's last elements come from the VEC that end with it, without a branch ahead of the load.
+template <typename T, int VEC, bool WHOLE> __device__ __forceinline__ void load_some(const T* row, int64_t c, int64_t len, float (&out)[VEC]) {
+  if constexpr (WHOLE) load<T, VEC>(row + c, out);
+  else {
+    static_assert(sizeof(T) * VEC == 16, "16 bytes");
+    typedef unsigned __int128 u128;
+    u128 v = 0;
+    if (len >= VEC) {
+      __builtin_memcpy(&v, row + min(c, len - VEC), 16);
+      if (c + VEC > len) v >>= 8 * (int)sizeof(T) * (int)(c + VEC - len);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        if (i < len) {
+          T x;
+          x = row[i];
+          uint32_t bits = 0;
+          __builtin_memcpy(&bits, &x, sizeof(T));
+          v |= (u128)bits << (8 * (int)sizeof(T) * i);
+        }
+      }
+    }
+    T e[VEC];
+    __builtin_memcpy(e, &v, 16);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) out[i] = up(e[i]);
+  }
+}
+template <typename T, int VEC, bool WHOLE> __device__ __forceinline__ void put_some(T* p, int64_t n, const T (&v)[VEC]) {
+  if constexpr (WHOLE) {
+    Group<T, VEC> g;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) g.v[i] = v[i];
+    *reinterpret_cast<Group<T, VEC>*>(p) = g;
+  } else if (n >= VEC) __builtin_memcpy(p, v, sizeof(v));
+  else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (i < n) p[i] = v[i];
+  }
+}
+template <typename T, int VEC, bool WHOLE> __device__ __forceinline__ void store_some(T* p, int64_t n, const float (&in)[VEC]) {
+  T v[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) v[i] = down<T>(in[i]);
+  put_some<T, VEC, WHOLE>(p, n, v);
+}
+
 // A lane of a product's tile holds four consecutive 16-bit values (two words) of a row, its row's other 16-lane groups the next ones, and the values
 // 16 further on are in the next fragment.  `a` and `b` are two such fragments: afterwards the lane holds eight consecutive values, `a` then `b`, at
 // 16 * (group / 2) + 8 * (group % 2) from the first fragment's start, so that a store writes 64 bytes of each of 16 rows instead of 32.
