@@ -83,7 +83,7 @@ int64_t simple_embed_grad_workspace(int64_t T, int64_t V, int64_t D);
  * The head in 8 bits: out[t, v] = (sum over k of codes[t, k] * w_codes[v, k]) * scales[t] * w_scales[v] for T tokens, V channels and rows
  * of K codes (K <= 131071, so that the 32-bit sums cannot overflow; they are exact).  Scales are float32, one rounding to out_dtype.
  * The output is a logits matrix as simple_sample reads it.  T <= 2^24, V <= 2^28.  workspace_dev (16-byte aligned,
- * simple_linear_int8_workspace() bytes) serves calls of more than 128 tokens whose codes' rows are not all 16-byte aligned multiples of 16;
+ * simple_linear_int8_workspace() bytes) serves calls of more than 512 tokens whose codes' rows are not all 16-byte aligned multiples of 16;
  * it may be NULL, which makes those slower.
  */
 int simple_linear_int8(const int8_t* codes_dev, int64_t code_stride, const float* scales_dev, const int8_t* w_codes_dev, int64_t w_code_stride,

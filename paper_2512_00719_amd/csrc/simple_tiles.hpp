@@ -397,9 +397,9 @@ __device__ __forceinline__ void planned(const Operand& P, const Operand& Q, int 
 }
 
 // Rows of any alignment, copied to rows of `out_stride` bytes (a multiple of 16), zeros behind their end.  Many tokens read a weight
-// row often: with rows that start anywhere staged through registers, 2000 tokens x 50,001 x 1023 bfloat16 took 514 us, and 204 + 45 for
-// the copy so; up to FEW_TOKENS the copy costs what it saves.
-constexpr int64_t FEW_TOKENS = 128;
+// row often, few do not repay the copy: scored against 50,001 x 1023 bfloat16 2000 tokens take 234 us with copies and 286 without, 1000 147 and 160; against
+// 100,000 x 1023 512 take 188 and 178, 256 150 and 112; of the 8-bit head's 100,000 x 2047 1000 take 299 and 353, 500 197 and 195, 200 149 and 118.
+constexpr int64_t FEW_TOKENS = 512;
 constexpr int64_t ALIGN_ROWS = 65536;  // weights at a time
 template <int BYTES> __global__ __launch_bounds__(256) void align_kernel(const unsigned char* in, int64_t stride, int64_t rows, int64_t bytes, unsigned char* out,
                                                                          int64_t out_stride) {

@@ -226,8 +226,9 @@ def linear_int8(codes, scales, w_codes, w_scales, *, out_dtype: torch.dtype = to
     if out_dtype not in _TYPES:
         raise TypeError(f"logits are float32 or bfloat16, got {out_dtype}")
     out = _out(out, "out", (T, V), out_dtype, codes.device)
-    rows = codes.data_ptr() | w_codes.data_ptr() | _stride(codes) | _stride(w_codes) | K
-    ws = _workspace(_lib.simple_linear_int8_workspace(T, V, K), "simple_linear_int8_workspace", codes.device) if T > 128 and rows % 16 else None
+    ws = None
+    if (codes.data_ptr() | w_codes.data_ptr() | _stride(codes) | _stride(w_codes) | K) % 16:  # rows that are not aligned
+        ws = _workspace(_lib.simple_linear_int8_workspace(T, V, K), "simple_linear_int8_workspace", codes.device)
     _check(_lib.simple_linear_int8(codes.data_ptr(), _stride(codes), scales.data_ptr(), w_codes.data_ptr(), _stride(w_codes), w_scales.data_ptr(),
                                    T, V, K, out.data_ptr(), _stride(out), _TYPES[out_dtype], _ptr(ws), 0 if ws is None else ws.numel(),
                                    _current_stream()), "simple_linear_int8")

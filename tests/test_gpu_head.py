@@ -84,3 +84,10 @@ def test_norm_head_and_sampling_call_together():
     ids = s.sample(logits, params, seed=1, step=0)
     assert torch.equal(ids.long(), logits.argmax(1))
     s.close()
+
+
+def test_copies_with_aligned_rows_in_more_than_one_piece():
+    """More than 512 tokens and 65,536 channels, rows of 33 codes: the weights are copied a piece at a time."""
+    from paper_2512_00719_amd import vocab
+    a, sa, b, sb = _inputs(520, 66_000, 33, 3)
+    _check(vocab.linear_int8(a, sa, b, sb), _want(a, sa, b, sb), F32)

@@ -187,3 +187,16 @@ def test_no_tokens():
     dh, dw = vocab.linear_xent_grad(f, h, w, y, f, dweight=w.clone())
     assert dh.shape == (0, 24) and not dw.any()
     assert torch.equal(vocab.linear_xent_grad(f, h, w, y, f, dweight=w.clone(), accumulate=True)[1], w)
+
+
+def test_copies_with_aligned_rows_in_more_than_one_piece():
+    """More than 512 tokens and 65,536 rows of 19 values: the weights are copied a piece at a time, forward and for the gradient."""
+    from paper_2512_00719_amd import vocab
+    h, w, y, dl = _inputs(530, 66_000, 19, 6)
+    want = _formula(h, w, y, dl, 1.0)
+    loss, lse = vocab.linear_xent(h, w, y)
+    _check(lse, want["lse"], "lse")
+    _check(loss, want["loss"], "loss")
+    dh, dw = vocab.linear_xent_grad(dl, h, w, y, lse)
+    _check(dh, want["dh"], "dh")
+    _check(dw, want["dw"], "dw", BF16)

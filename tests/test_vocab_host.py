@@ -61,8 +61,8 @@ def test_head_refusals():
         a, as_, sa, b, bs, sb, T, V, K, o, os_, t, ws, n, 0)
     assert (head(a=0) == head(sa=0) == head(b=0) == head(sb=0) == head(o=0) == head(as_=7) == head(bs=7) == head(os_=4) == head(T=-1) == head(V=0) ==
             head(K=0) == head(t=2) == head(ws=X + 8) == INVALID)
-    need = lib.simple_linear_int8_workspace(200, 5, 8)
-    assert need > 0 and head(T=200, ws=X, n=need - 1) == CAPACITY and lib.simple_linear_int8_workspace(200, 0, 8) == INVALID
+    need = lib.simple_linear_int8_workspace(600, 5, 8)
+    assert need > 0 and head(T=600, ws=X, n=need - 1) == CAPACITY and lib.simple_linear_int8_workspace(200, 0, 8) == INVALID
     assert head(K=131_072, as_=131_072, bs=131_072) == CAPACITY
     assert head(T=0, a=0, o=0) == OK
 
