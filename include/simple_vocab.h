@@ -96,7 +96,8 @@ int64_t simple_linear_int8_workspace(int64_t T, int64_t V, int64_t K);
  * matrix is kept:
  *   lse[t] = log(sum over v of exp z[t, v]),   loss[t] = lse[t] - z[t, targets[t]]
  * loss is the negative log-probability of the target, 0 where the target is outside [0, V) (a token that is masked).  logit_scale (positive) is
- * 1 / temperature for tokens that were drawn at one.  workspace_dev: simple_xent_workspace(T, V, D) bytes, 16-byte aligned.  T <= 2^20, V <= 2^28, D <= 65536.
+ * 1 / temperature for tokens that were drawn at one.  workspace_dev: simple_xent_workspace(T, V, D) bytes, 16-byte aligned.  T <= 2^20, V <= 2^28, D <= 65536, and
+ * T * V < 2^41.
  */
 int simple_xent(const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, const int32_t* targets_dev,
                 int64_t T, int64_t V, int64_t D, float logit_scale, float* loss_dev, float* lse_dev, void* workspace_dev,

@@ -95,12 +95,7 @@ template <class S, bool DIRECT> void launch(Args a, hipStream_t st) {
   }
 }
 template <bool DIRECT> void launch_for(const Args& a, hipStream_t st) {
-  const int64_t T = a.tokens.rows;
-  if (T <= 16) launch<Shape<Int8, 16, 64, 1, 4, 4>, DIRECT>(a, st);
-  else if (T <= 32) launch<Shape<Int8, 32, 64, 1, 4, 4>, DIRECT>(a, st);
-  else if (T <= 64) launch<Shape<Int8, 64, 64, 1, 4, 4>, DIRECT>(a, st);
-  else if (T <= 128) launch<Shape<Int8, 128, 128, 2, 2, 2>, DIRECT>(a, st);
-  else launch<Shape<Int8, 256, 256, 2, 4, 2>, DIRECT>(a, st);
+  shaped<Int8>(tiles_for(a.tokens.rows, a.weights.rows), [&](auto shape) { launch<decltype(shape), DIRECT>(a, st); });
 }
 
 }  // namespace head

@@ -196,6 +196,14 @@ __global__ __launch_bounds__(NT > WG ? NT : WG) void grad_kernel(GradArgs a) {
         }
       }
     }
+    if constexpr (!WHOLE) {  // a row's last group overlaps its neighbour's: dh, where dx goes in its place, is here before anything is written
+      if (a.dh) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) asm volatile("" : "+v"(e[i][j]));
+      }
+    }
     row_reduce<NT>(sum, none, part[turn & 1]);  // (two areas in turn: one barrier a row)
     ++turn;
     const float m = sum / (float)a.D;

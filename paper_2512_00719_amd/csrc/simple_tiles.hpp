@@ -396,6 +396,28 @@ __device__ __forceinline__ void planned(const Operand& P, const Operand& Q, int 
   }, [&](auto& acc, int64_t p0, int64_t q0) { done(S{}, acc, p0, q0); });
 }
 
+// Shapes by the number of P's rows.  Few read every row of Q once, in four stages that keep the memory busy.  Many run at the matrix rate, in the tiles that
+// take fewer rounds: one of 256 x 256 a compute unit, or two of 128 x 128, at 0.8 of the rate (256 tokens x 32,000 x 4096 int8: 125 of the one kind
+// leave half of the chip idle).
+enum { TILE_16, TILE_32, TILE_64, TILE_128, TILE_256 };
+inline int tiles_for(int64_t p, int64_t q) {
+  if (p <= 16) return TILE_16;
+  if (p <= 32) return TILE_32;
+  if (p <= 64) return TILE_64;
+  if (p <= 128) return TILE_128;
+  const int64_t large = ceil_div(p, 256) * ceil_div(q, 256), small = ceil_div(p, 128) * ceil_div(q, 128), last = large % CUS;
+  const double rounds = (double)(large / CUS) + (last == 0 ? 0.0 : last * 4 <= CUS ? 0.35 : 1.0);
+  return rounds <= 0.625 * (double)ceil_div(small, 2 * CUS) ? TILE_256 : TILE_128;
+}
+inline int64_t tile_columns(int tiles) { return tiles <= TILE_64 ? 64 : tiles == TILE_128 ? 128 : 256; }
+template <class E, typename F> void shaped(int tiles, F&& f) {
+  if (tiles == TILE_16) f(Shape<E, 16, 64, 1, 4, 4>{});
+  else if (tiles == TILE_32) f(Shape<E, 32, 64, 1, 4, 4>{});
+  else if (tiles == TILE_64) f(Shape<E, 64, 64, 1, 4, 4>{});
+  else if (tiles == TILE_128) f(Shape<E, 128, 128, 2, 2, 2>{});
+  else f(Shape<E, 256, 256, 2, 4, 2>{});
+}
+
 // Rows of any alignment, copied to rows of `out_stride` bytes (a multiple of 16), zeros behind their end.  Many tokens read a weight
 // row often, few do not repay the copy: scored against 50,001 x 1023 bfloat16 2000 tokens take 234 us with copies and 286 without, 1000 147 and 160; against
 // 100,000 x 1023 512 take 188 and 178, 256 150 and 112; of the 8-bit head's 100,000 x 2047 1000 take 299 and 353, 500 197 and 195, 200 149 and 118.

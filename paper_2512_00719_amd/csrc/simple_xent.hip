@@ -505,16 +505,6 @@ __global__ __launch_bounds__(64 * HID_GROUPS) void hidden_kernel(const float* su
   }
 }
 
-// Tiles by the number of tokens: few tokens read every weight row once, in four stages that keep the memory busy; many run at the matrix rate.
-template <class E, typename F> void shaped(int64_t T, F&& f) {
-  if (T <= 16) f(Shape<E, 16, 64, 1, 4, 4>{});
-  else if (T <= 32) f(Shape<E, 32, 64, 1, 4, 4>{});
-  else if (T <= 64) f(Shape<E, 64, 64, 1, 4, 4>{});
-  else if (T <= 128) f(Shape<E, 128, 128, 2, 2, 2>{});
-  else f(Shape<E, 256, 256, 2, 4, 2>{});
-}
-int64_t tile_q(int64_t T) { return T <= 64 ? 64 : T <= 128 ? 128 : 256; }
-
 constexpr int SHORT_K = 4 * KB;
 constexpr int64_t PIECE = (int64_t)1 << 27;   // values of G kept at a time (256 MB in each order)
 constexpr int64_t ROUND = 256;                // a piece's rows: a multiple of every tile
@@ -526,7 +516,7 @@ int64_t piece_rows(int64_t T, int64_t V) {
 // Workgroups a tile of dH: enough to fill the chip, each with at least 16 steps of k.
 int hidden_splits(int64_t T, int64_t V, int64_t D) {
   const int64_t bp = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : 256;
-  const int64_t tiles = std::max<int64_t>(1, ceil_div(T, bp) * ceil_div(D, tile_q(T))), want = T <= 64 ? 1024 : T <= 128 ? 512 : 256;
+  const int64_t tiles = std::max<int64_t>(1, ceil_div(T, bp) * ceil_div(D, T <= 64 ? 64 : T <= 128 ? 128 : 256)), want = T <= 64 ? 1024 : T <= 128 ? 512 : 256;
   const int64_t most = std::max<int64_t>(1, piece_rows(T, V) * 2 / (16 * KB));
   return (int)std::max<int64_t>(1, std::min(most, want / tiles));
 }
@@ -572,7 +562,8 @@ void multiply(MulArgs a, int type, bool add, int splits, hipStream_t st) {
   a.vec = rows_aligned(a.out, a.stride, type_bytes(type), 16);
   // (Few steps of k, as dW of few tokens has: a tile is mostly stored, and two smaller ones on a compute unit do so in turn.)
   // (So too where a tile of 256 columns would be half empty.)
-  shaped<F16>(a.k_bytes <= SHORT_K || a.q.rows <= 128 ? std::min<int64_t>(a.p.rows, 128) : a.p.rows, [&](auto shape) {
+  const int tiles = tiles_for(a.p.rows, a.q.rows);
+  shaped<F16>(a.k_bytes <= SHORT_K || a.q.rows <= 128 ? std::min<int>(tiles, TILE_128) : splits > 1 && a.p.rows > 128 ? TILE_256 : tiles, [&](auto shape) {
     using S = decltype(shape);
     a.plan = plan<S, Cut<S>::CAN>(a.p.rows, a.q.rows, splits == 1);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)a.plan.grid, (unsigned)splits), dim3(S::THREADS), 0, st, a); };
@@ -594,7 +585,9 @@ int check_sizes(int64_t T, int64_t V, int64_t D) {
   return T > MAX_T || V > MAX_V || D > MAX_D ? SIMPLE_ECAPACITY : SIMPLE_OK;
 }
 bool good_scale(float s) { return s > 0.f && s <= 3.4e38f; }
-int64_t pairs_bytes(int64_t T, int64_t V) { return ((ceil_div(V, tile_q(T)) * T * (int64_t)sizeof(Pair) + 255) & ~(int64_t)255); }
+// (Tiles are numbered in 32 bits.)
+bool too_many_tiles(int64_t T, int64_t V) { return ceil_div(T, 16) * ceil_div(V, 64) > (int64_t)0x7FFFFFFF; }
+int64_t pairs_bytes(int64_t T, int64_t V) { return ((ceil_div(V, tile_columns(tiles_for(T, V))) * T * (int64_t)sizeof(Pair) + 255) & ~(int64_t)255); }
 }  // namespace
 
 extern "C" int64_t simple_xent_workspace(int64_t T, int64_t V, int64_t D) {
@@ -613,7 +606,7 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
   if (T == 0) return SIMPLE_OK;
   if (!hidden_dev || !weight_dev || !targets_dev || !loss_dev || !lse_dev) return SIMPLE_EINVAL;
   if (!workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
-  if (workspace_bytes < simple_xent_workspace(T, V, D)) return SIMPLE_ECAPACITY;
+  if (too_many_tiles(T, V) || workspace_bytes < simple_xent_workspace(T, V, D)) return SIMPLE_ECAPACITY;
   hipStream_t st = (hipStream_t)hip_stream;
   unsigned char* ws = (unsigned char*)workspace_dev;
   Args a{};
@@ -624,12 +617,13 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
   a.targets = targets_dev;
   a.V = V;
   a.at_target = (float*)(ws + pairs_bytes(T, V));
-  const int64_t tiles_q = ceil_div(V, tile_q(T));
+  const int tiles = tiles_for(T, V);
+  const int64_t columns = tile_columns(tiles), tiles_q = ceil_div(V, columns);
   auto stats = [&](const Operand& w, int64_t v0, bool dir) {
     a.weight = w;
     a.v0 = v0;
-    a.pairs = (Pair*)ws + v0 / tile_q(T) * T;
-    shaped<Bf16>(T, [&](auto shape) {
+    a.pairs = (Pair*)ws + v0 / columns * T;
+    shaped<Bf16>(tiles, [&](auto shape) {
       using S = decltype(shape);
       a.plan = plan<S, false>(T, w.rows);
       const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
@@ -672,7 +666,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   const Layout L = layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr);
   if (T > 0) {
     if (!dloss_dev || !hidden_dev || !weight_dev || !targets_dev || !lse_dev || !workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
-    if (workspace_bytes < L.total) return SIMPLE_ECAPACITY;
+    if (too_many_tiles(T, V) || workspace_bytes < L.total) return SIMPLE_ECAPACITY;
   }
   unsigned char* ws = (unsigned char*)workspace_dev;
   Args a{};
@@ -712,7 +706,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
     if (copies) a.weight = aligned_copy<2>(a.weight, D * 2, ws + L.copy_w, st);
     if (T > 0) {
       const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
-      shaped<Bf16>(T, [&](auto shape) {
+      shaped<Bf16>(tiles_for(T, n), [&](auto shape) {
         using S = decltype(shape);
         a.plan = plan<S, false>(T, n);
         const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
