@@ -28,12 +28,12 @@ template <typename T, bool VEC> __device__ __forceinline__ void put4(T* to, int6
   }
 }
 
-template <class S> constexpr bool many = Cut<S>::CAN;
+template <class S, bool DIRECT> constexpr bool many = DIRECT && Cut<S>::CAN;  // (staged through registers as well, the products' own would spill)
 
 template <class S, bool DIRECT, typename T, bool VEC>
 __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
   __shared__ __align__(1024) unsigned char lds[S::LDS];
-  planned<S, DIRECT, many<S>>(a.tokens, a.weights, a.k_bytes, a.plan, lds, [&](auto shape, auto& acc, int64_t p0, int64_t q0) {
+  planned<S, DIRECT, many<S, DIRECT>>(a.tokens, a.weights, a.k_bytes, a.plan, lds, [&](auto shape, auto& acc, int64_t p0, int64_t q0) {
     using R = decltype(shape);
     const int lane = opaque_lane(), wave = threadIdx.x >> 6;
     const int64_t p1 = p0 + wave % R::NWP * R::FP * 16 + (lane & 15), q1 = q0 + wave / R::NWP * R::FQ * 16 + (lane >> 4) * 4;
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
 }
 
 template <class S, bool DIRECT> void launch(Args a, hipStream_t st) {
-  a.plan = plan<S, many<S>>(a.tokens.rows, a.weights.rows);
+  a.plan = plan<S, many<S, DIRECT>>(a.tokens.rows, a.weights.rows);
   const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
   if (a.out_type == SIMPLE_F32) {
     if (a.vec) hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float, true>), grid, block, 0, st, a);

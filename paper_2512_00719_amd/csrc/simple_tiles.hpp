@@ -77,6 +77,13 @@ __device__ __forceinline__ i32x4 resource_of(const Operand& o, int64_t row0, int
 }
 
 
+// The lane, hidden from the optimiser, which would otherwise keep what follows from it in registers through the products.
+__device__ __forceinline__ int opaque_lane() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
 // A workgroup's tile, its waves (NWP along P times NWQ along Q), and how many steps are staged at once.
 template <class E_, int BP_, int BQ_, int NWP_, int NWQ_, int STAGES_> struct Shape {
   using E = E_;
@@ -106,12 +113,6 @@ __device__ __forceinline__ int place_of(int id, int n) {
 // on from a tile to the next while the finished one is stored.  (Smaller tiles, several of them on a compute unit, are left to the dispatcher, one a
 // workgroup: taken in rounds, one token against 128,256 x 4096 int8 weights took 117 us, 92 so.)  Tiles of a last round that is at most a quarter full are cut in
 // four along P instead, eight waves to each part, a workgroup to each: the round then takes about 0.35 of a whole one.
-// (The lane as done() has it: hidden from the optimiser, which would otherwise keep what follows from it in registers through the products.)
-__device__ __forceinline__ int opaque_lane() {
-  int lane = threadIdx.x & 63;
-  asm volatile("" : "+v"(lane));
-  return lane;
-}
 template <typename T> __device__ __forceinline__ void arrived_value(T& v) { asm volatile("" : "+v"(v)); }
 template <class S> struct Cut {
   static constexpr bool CAN = S::BP == 256 && S::BQ == 256;
@@ -152,8 +153,9 @@ __device__ __forceinline__ i32x4 taken_from(u128 v, int k, int k_bytes) {
 template <class S> struct Loader {
   i32x4 res_p, res_q;
   uint32_t off_p[S::LP], off_q[S::LQ];
-  int wave, chunk, row8, k_bytes;
-  __device__ __forceinline__ void to(const Operand& P, const Operand& Q, int64_t p0, int64_t q0) {
+  int wave;
+  __device__ __forceinline__ void to(const Operand& P, const Operand& Q, int64_t p0, int64_t q0, int k_bytes) {
+    const int lane = opaque_lane(), row8 = lane >> 3, chunk = (lane & 7) ^ row8;  // what a lane stages of its group of 8 rows
     res_p = resource_of(P, p0, S::BP, k_bytes);
     res_q = resource_of(Q, q0, S::BQ, k_bytes);
     const int p_rows = (int)min((int64_t)S::BP, P.rows - p0), q_rows = (int)min((int64_t)S::BQ, Q.rows - q0);
@@ -162,12 +164,21 @@ template <class S> struct Loader {
 #pragma unroll
     for (int i = 0; i < S::LQ; ++i) off_q[i] = (uint32_t)min((wave + i * S::NW) % S::GQ * 8 + row8, q_rows - 1) * (uint32_t)Q.stride + chunk * 16;
   }
+  // Ahead of the last step's loads: chunks behind the rows' end go behind the resources' end, which reads as zeros.
+  __device__ __forceinline__ void end_at(int left) {
+    const int lane = opaque_lane(), chunk = (lane & 7) ^ (lane >> 3);
+    if (chunk * 16 >= left) {
+#pragma unroll
+      for (int i = 0; i < S::LP; ++i) off_p[i] = 0x80000000u;
+#pragma unroll
+      for (int i = 0; i < S::LQ; ++i) off_q[i] = 0x80000000u;
+    }
+  }
   // load n of step s: the LP of P, then the LQ of Q
   __device__ __forceinline__ void load(int s, uint32_t stage, int n) const {
     const uint32_t k = (uint32_t)s * KB;
-    const bool behind = (int)k + chunk * 16 >= k_bytes;  // behind the row's end: an address behind the resource's, which reads as zeros
-    if (n < S::LP) to_lds(stage + (wave + n * S::NW) % S::GP * 1024, behind ? 0x80000000u : off_p[n], res_p, k);
-    else to_lds(stage + S::BP * KB + (wave + (n - S::LP) * S::NW) % S::GQ * 1024, behind ? 0x80000000u : off_q[n - S::LP], res_q, k);
+    if (n < S::LP) to_lds(stage + (wave + n * S::NW) % S::GP * 1024, off_p[n], res_p, k);
+    else to_lds(stage + S::BP * KB + (wave + (n - S::LP) * S::NW) % S::GQ * 1024, off_q[n - S::LP], res_q, k);
   }
 };
 
@@ -182,7 +193,6 @@ __device__ __forceinline__ void products(const Operand& P, const Operand& Q, int
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % S::NWP, wq = wave / S::NWP;
   const int steps = (k_bytes + KB - 1) / KB;
-  const int row8 = lane >> 3, chunk = (lane & 7) ^ row8;  // what a lane stages of its group of 8 rows
   typename S::Acc acc[S::FQ][S::FP];
   auto clear = [&] {
 #pragma unroll
@@ -229,14 +239,16 @@ __device__ __forceinline__ void products(const Operand& P, const Operand& Q, int
     constexpr int NL = S::LP + S::LQ;
     // the step that is loaded next: step ls of tile lt, if there is one
     Loader<S> from;
-    from.wave = wave; from.chunk = chunk; from.row8 = row8; from.k_bytes = k_bytes;
+    from.wave = wave;
     int lt = 0, ls = 0;
     bool more;
+    const int left = k_bytes - (steps - 1) * KB;  // bytes of the last step
     {
       int64_t lp, lq;
       more = tile(0, lp, lq);
       if (!more) return;
-      from.to(P, Q, lp, lq);
+      from.to(P, Q, lp, lq, k_bytes);
+      if (steps == 1 && left < KB) from.end_at(left);
     }
     auto onward = [&] {
       if (++ls == steps) {
@@ -245,9 +257,10 @@ __device__ __forceinline__ void products(const Operand& P, const Operand& Q, int
           ls = 0;
           int64_t lp, lq;
           more = tile(++lt, lp, lq);
-          if (more) from.to(P, Q, lp, lq);
+          if (more) from.to(P, Q, lp, lq, k_bytes);
         }
       }
+      if (ls == steps - 1 && left < KB && more) from.end_at(left);
     };
     auto issue = [&](int stage) {
 #pragma unroll
@@ -320,6 +333,7 @@ __device__ __forceinline__ void products(const Operand& P, const Operand& Q, int
       }
     }
   } else {
+    const int row8 = lane >> 3, chunk = (lane & 7) ^ row8;  // what a lane stages of its group of 8 rows
     for (int n = 0; tile(n, p0, q0); ++n) {
       const int p_rows = (int)min((int64_t)S::BP, P.rows - p0), q_rows = (int)min((int64_t)S::BQ, Q.rows - q0);
       const unsigned char *row_p[S::LP], *row_q[S::LQ];
