@@ -107,7 +107,7 @@ int64_t simple_xent_workspace(int64_t T, int64_t V, int64_t D);
 /*
  * Its gradient for a loss of sum over t of dloss[t] * loss[t]: with G[t, v] = logit_scale * dloss[t] * (exp(z[t, v] - lse[t]) - [v = targets[t]]),
  *   dhidden = G * weight (bfloat16),   dweight = transposed G * hidden (dweight_dtype; accumulate != 0 adds it to what is there)
- * lse_dev is what simple_xent wrote.  Logits are formed again, a piece of the vocabulary at a time, and G is rounded to 11 bits for the products.
+ * lse_dev is what simple_xent wrote.  Logits are formed again, a piece of the vocabulary at a time, and G is rounded to 11 bits or more for the products.
  * A token whose target is outside [0, V) or whose dloss is 0 takes no part whatever its states hold: its row of dhidden is zeros.
  * Either output may be NULL: then it is not formed.  workspace_dev: simple_xent_grad_workspace() bytes for the outputs wanted, 16-byte aligned.
  */

@@ -47,6 +47,8 @@ struct Args {
   const struct Token* tokens;
   uint16_t *g, *gt;        // [T][g_stride], [rows of the piece][gt_stride]; either may be null
   int64_t g_stride, gt_stride;
+  const float *lse, *dloss;  // of few tokens, who have no Token
+  int64_t g_plane, gt_plane;
 };
 
 template <class S> constexpr int stats_room = S::BP * S::NWQ * (int)sizeof(Pair);  // (a cut tile's parts need a half of it)
@@ -149,6 +151,8 @@ __global__ __launch_bounds__(FIN_T * FIN_GROUPS) void finish_kernel(const Pair* 
   }
 }
 
+__device__ __forceinline__ bool takes_part(int32_t target, float dloss, int64_t V) { return target >= 0 && target < V && dloss != 0.f; }
+
 // What the gradient knows of a token: its target (-1: it takes no part), lse, the power of two on its row of G, and what the row still lacks of
 // the gradient, c dl over that power.
 struct Token { int32_t y; float lse, up, rest; };
@@ -197,7 +201,7 @@ __global__ __launch_bounds__(256) void prepare_kernel(PrepareArgs a) {
     const int64_t t = (int64_t)blockIdx.x * 4 + wave;
     const int32_t y = t < a.T ? a.targets[t] : -1;
     const float dl = t < a.T ? a.dloss[t] : 0.f;
-    const bool on = y >= 0 && y < a.V && dl != 0.f;
+    const bool on = takes_part(y, dl, a.V);
     Token k{-1, 0.f, 1.f, 0.f};
     if (on) {
       const uint16_t *h = a.hidden + t * a.hidden_stride, *w = a.weight + y * a.weight_stride;
@@ -272,7 +276,8 @@ __global__ __launch_bounds__(1024) void tops_kernel(const float* partial, int to
 __device__ __forceinline__ uint32_t f16_bits(float f) { return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)f); }
 
 // G of a tile, in both orders.  Columns behind the piece's last and tokens behind the last are zeros: sums run over them.
-template <class S>
+// FEW: the gradient itself, as the sum of two bfloat16 values in planes of their own.
+template <class S, bool FEW>
 __device__ __forceinline__ void g_of(const Args& a, typename S::Acc (&acc)[S::FQ][S::FP], int64_t p0, int64_t q0, unsigned char* lds) {
   const int64_t T = a.hidden.rows;
   const int lane = opaque_lane(), wave = threadIdx.x >> 6, wp = wave % S::NWP, wq = wave / S::NWP;
@@ -291,7 +296,12 @@ __device__ __forceinline__ void g_of(const Args& a, typename S::Acc (&acc)[S::FQ
   for (int j = 0; j < S::FP; ++j) {
     const int pl = (wp * S::FP + j) * 16 + (lane & 15);
     const int64_t p = p0 + pl;
-    const Token k = p < T ? a.tokens[p] : Token{-1, 0.f, 1.f, 0.f};
+    Token k{-1, 0.f, 1.f, 0.f};
+    if constexpr (FEW) {
+      if (p < T && takes_part(a.targets[p], a.dloss[p], a.V)) k = Token{a.targets[p], a.lse[p], a.dloss[p] * a.scale, 0.f};
+    } else {
+      if (p < T) k = a.tokens[p];
+    }
     const int64_t target = (int64_t)k.y - a.v0 - q1;
     const bool here = k.y >= 0 && target >= 0 && target < S::FQ * 16;
     constexpr int PAIR = S::FQ % 2 == 0 ? 2 : 1;
@@ -310,8 +320,23 @@ __device__ __forceinline__ void g_of(const Args& a, typename S::Acc (&acc)[S::FQ
             if (target == i * 16 + e) f[e] -= 1.f;
         }
         uint32_t v[4];
+        if constexpr (FEW) {
+          uint32_t low[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits(f[e] * k.up) : 0u;
+          for (int e = 0; e < 4; ++e) {
+            const float x = k.y >= 0 && i * 16 + e < left ? f[e] * k.up : 0.f;
+            v[e] = to_bf16(x);
+            low[e] = to_bf16(x - up((uint16_t)v[e]));
+          }
+          if (a.g && p < T) *reinterpret_cast<uint2*>(a.g + a.g_plane + p * a.g_stride + q1 + i * 16) = uint2{low[0] | low[1] << 16, low[2] | low[3] << 16};
+          if (a.gt && p < a.gt_stride) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a.gt[a.gt_plane + (q1 + i * 16 + e) * a.gt_stride + p] = (uint16_t)low[e];
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = k.y >= 0 && i * 16 + e < left ? f16_bits(f[e] * k.up) : 0u;
+        }
         word[n] = uint2{v[0] | v[1] << 16, v[2] | v[3] << 16};
         if constexpr (TURN) {
           if (a.gt) {
@@ -349,11 +374,11 @@ __device__ __forceinline__ void g_of(const Args& a, typename S::Acc (&acc)[S::FQ
     }
   }
 }
-template <class S, bool DIRECT>
+template <class S, bool DIRECT, bool FEW>
 __global__ __launch_bounds__(S::THREADS) void g_kernel(Args a) {
   __shared__ __align__(1024) unsigned char lds[S::LDS];
   planned<S, DIRECT, false>(a.hidden, a.weight, a.k_bytes, a.plan, lds,
-                            [&](auto shape, auto& acc, int64_t p0, int64_t q0) { g_of<decltype(shape)>(a, acc, p0, q0, lds); });
+                            [&](auto shape, auto& acc, int64_t p0, int64_t q0) { g_of<decltype(shape), FEW>(a, acc, p0, q0, lds); });
 }
 
 // out[c][r] = in[r][c], from bfloat16 to 16-bit floats of 11 bits in range: rows behind the last and rows of tokens that take no part are zeros,
@@ -467,18 +492,18 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
 constexpr int HID_GROUPS = 4;
 template <int VEC>
 __global__ __launch_bounds__(64 * HID_GROUPS) void hidden_kernel(const float* sums, int splits, int64_t T, int64_t D, const Token* tokens, const uint32_t* top,
-                                                                 uint16_t* out, int64_t stride) {
+                                                                 const int32_t* targets, const float* dloss, int64_t V, uint16_t* out, int64_t stride) {
   __shared__ float part[HID_GROUPS][64 * VEC];
   const int64_t t = blockIdx.x;
-  const Token k = tokens[t];
-  const float m = k.rest * from_range(*top);
+  const bool on = takes_part(targets[t], dloss[t], V);
+  const float m = tokens ? tokens[t].rest * from_range(*top) : 1.f;
   const bool shared_out = splits > 1;
   const int lane = threadIdx.x & 63, grp = threadIdx.x >> 6;
   const int64_t c = shared_out ? ((int64_t)blockIdx.y * 64 + lane) * VEC : ((int64_t)blockIdx.y * (64 * HID_GROUPS) + threadIdx.x) * VEC;
   float v[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) v[e] = 0.f;
-  if (c < D && k.y >= 0) {
+  if (c < D && on) {
     const float* p = sums + t * D + c;
 #pragma unroll 8
     for (int s = shared_out ? grp : 0; s < splits; s += HID_GROUPS) {
@@ -500,8 +525,179 @@ __global__ __launch_bounds__(64 * HID_GROUPS) void hidden_kernel(const float* su
   }
   if (c < D) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) v[e] = k.y >= 0 ? v[e] * m : 0.f;
+    for (int e = 0; e < VEC; ++e) v[e] = on ? v[e] * m : 0.f;
     store<uint16_t, VEC>(out + t * stride + c, v);
+  }
+}
+
+// ---- few tokens: the weights are what is read, and each product takes them as they lie ----
+// G is the sum of two bfloat16 values, 16 bits that need no range, so that neither weights nor states are copied into another type; twice the matrix
+// instructions are free where the memory is the bound.
+constexpr int64_t FEW_GRAD = 64;
+constexpr int FEW_STAGES = 3, FEW_K = 64;  // rows of the weights a step
+
+// Fragments with k across an LDS tile's rows: each 16 lanes are given 4 rows of 16 values, and a lane gets its column's four.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x4 turned(const unsigned char* rows0, const unsigned char* rows4) {
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(s16x4*)rows0), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(s16x4*)rows4);
+  const int2 x = __builtin_bit_cast(int2, a), y = __builtin_bit_cast(int2, b);
+  return i32x4{x.x, x.y, y.x, y.y};
+}
+
+struct FewArgs {
+  Operand weight;          // the piece's rows
+  const uint16_t* g;       // two planes [T][g_stride]
+  int64_t g_stride, g_plane, T, D;
+  int split_rows;          // of the weights, a multiple of FEW_K
+  float* sums;             // [splits][T][D]
+  int add;
+};
+// sums[split][t][d] (+)= sum over the split's rows v of G[t][v] W[v][d]: a workgroup has 64 columns d, 16 a wave.  Bound: one read of the weights.
+template <int BP>
+__global__ __launch_bounds__(256) void dh_few_kernel(FewArgs a) {
+  constexpr int FP = BP / 16, W_BYTES = FEW_K * KB, STAGE = W_BYTES + 2 * BP * KB;
+  constexpr int GROUPS = 2 * BP / 8, LG = GROUPS / 4, NL = 2 + LG;  // loads a wave: its quarter of 8 + GROUPS groups of 8 rows
+  __shared__ __align__(1024) unsigned char lds[FEW_STAGES * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row8 = lane >> 3, chunk = (lane & 7) ^ row8;
+  const int64_t d0 = (int64_t)blockIdx.x * 64, v0 = (int64_t)blockIdx.y * a.split_rows;
+  const int rows = (int)max((int64_t)0, min((int64_t)a.split_rows, a.weight.rows - v0)), steps = (rows + FEW_K - 1) / FEW_K;
+  f32x4 acc[FP];
+#pragma unroll
+  for (int j = 0; j < FP; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const Operand g{(const unsigned char*)a.g, a.g_stride * 2, a.T};
+  const int g_bytes = (int)(a.g_stride * 2);
+  const i32x4 res_hi = resource_of(g, 0, BP, g_bytes), res_lo = resource_of(Operand{g.p + a.g_plane * 2, g.stride, g.rows}, 0, BP, g_bytes);
+  uint32_t off_w[2], off_g[LG];
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) off_w[i] = (uint32_t)((wave * 2 + i) * 8 + row8) * (uint32_t)a.weight.stride + (uint32_t)d0 * 2 + chunk * 16;
+#pragma unroll
+  for (int i = 0; i < LG; ++i) off_g[i] = (uint32_t)min(((wave * LG + i) * 8 + row8) % BP, (int)a.T - 1) * (uint32_t)g.stride + (uint32_t)v0 * 2 + chunk * 16;
+  auto issue = [&](int s, int stage) {
+    const uint32_t to = base + stage * STAGE;
+    // (rows behind the last read as zeros)
+    const i32x4 res_w = resource_of(a.weight, v0 + s * FEW_K, FEW_K, (int)(a.D * 2));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) to_lds(to + (wave * 2 + i) * 1024, off_w[i], res_w, 0u);
+#pragma unroll
+    for (int i = 0; i < LG; ++i) to_lds(to + W_BYTES + (wave * LG + i) * 1024, off_g[i], (wave * LG + i) * 8 < BP ? res_hi : res_lo, (uint32_t)s * KB);
+  };
+  const int i16 = lane & 15, grp = lane >> 4, w_chunk = wave * 2 + ((i16 & 3) >> 1);
+  const uint32_t at_w0 = (grp * 8 + i16 / 4) * KB + ((w_chunk ^ (i16 / 4)) << 4) + (i16 & 1) * 8;
+  const uint32_t at_w4 = (grp * 8 + 4 + i16 / 4) * KB + ((w_chunk ^ (4 + i16 / 4)) << 4) + (i16 & 1) * 8;
+  int in_flight = 0;
+  for (; in_flight < FEW_STAGES - 1 && in_flight < steps; ++in_flight) issue(in_flight, in_flight);
+  int stage = 0, next = in_flight;
+  for (int s = 0; s < steps; ++s) {
+    if (in_flight == FEW_STAGES - 1) arrived<(FEW_STAGES - 2) * NL>();
+    else arrived<0>();
+    if (next < steps) { issue(next, stage == 0 ? FEW_STAGES - 1 : stage - 1); ++next; }
+    else --in_flight;
+    const unsigned char* b = lds + stage * STAGE;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const i32x4 w = turned(b + at_w0 + h * 32 * KB, b + at_w4 + h * 32 * KB);
+      const uint32_t c = (uint32_t)((h * 4 + grp) ^ (lane & 7)) * 16;
+#pragma unroll
+      for (int j = 0; j < FP; ++j) {
+        const unsigned char* r = b + W_BYTES + (j * 16 + i16) * KB + c;
+        acc[j] = Bf16::mma(w, *reinterpret_cast<const i32x4*>(r), acc[j]);
+        acc[j] = Bf16::mma(w, *reinterpret_cast<const i32x4*>(r + BP * KB), acc[j]);
+      }
+    }
+    stage = stage + 1 == FEW_STAGES ? 0 : stage + 1;
+  }
+#pragma unroll
+  for (int j = 0; j < FP; ++j) {
+    const int64_t t = j * 16 + i16, d = d0 + wave * 16 + grp * 4;
+    if (t >= a.T || d >= a.D) continue;  // (D is a multiple of 8)
+    float* to = a.sums + ((int64_t)blockIdx.y * a.T + t) * a.D + d;
+    float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+    if (a.add) {
+      float o[4];
+      load<float, 4>(to, o);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += o[e];
+    }
+    store<float, 4>(to, v);
+  }
+}
+
+// States with tokens along the rows, [D][t_pad] bfloat16: zeros for tokens that take no part, and behind the last.
+__global__ __launch_bounds__(256) void states_few_kernel(const uint16_t* h, int64_t stride, int64_t T, int64_t D, int t_pad, const int32_t* targets, const float* dloss,
+                                                         int64_t V, uint16_t* out) {
+  const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int t0 = blockIdx.y * 8;
+  if (d >= D) return;
+  Group<uint16_t, 8> v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v.v[e] = t0 + e < T && takes_part(targets[t0 + e], dloss[t0 + e], V) ? h[(t0 + e) * stride + d] : (uint16_t)0;
+  *reinterpret_cast<Group<uint16_t, 8>*>(out + d * t_pad + t0) = v;
+}
+
+// dW[v][d] (+)= sum over the tokens of G[t][v] H[t][d]: a wave has 32 rows v, whose fragments stay in registers, against the columns d in turn, 32 at a time.  Nothing goes
+// through LDS: the states, [D][t_pad], come from the caches.  Bound: one write of the gradient.
+constexpr int FEW_COLUMNS = 256;
+template <int KS, typename T, bool ADD>
+__global__ __launch_bounds__(256) void dw_few_kernel(const uint16_t* gt, int64_t plane, const uint16_t* ht, int t_pad, int64_t n, int64_t D, T* out, int64_t stride,
+                                                     bool vec) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, grp = lane >> 4;
+  const int64_t v0 = ((int64_t)blockIdx.x * 4 + wave) * 32;
+  if (v0 >= n) return;
+  i32x4 hi[2][KS], lo[2][KS];
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const int t = k * 32 + grp * 8;
+      const uint16_t* row = gt + min(v0 + p * 16 + i16, n - 1) * t_pad + t;
+      hi[p][k] = lo[p][k] = i32x4{0, 0, 0, 0};
+      if (t < t_pad) {
+        hi[p][k] = *reinterpret_cast<const i32x4*>(row);
+        lo[p][k] = *reinterpret_cast<const i32x4*>(row + plane);
+      }
+    }
+  const int64_t d_end = min(D, ((int64_t)blockIdx.y + 1) * FEW_COLUMNS);
+#pragma unroll 2
+  for (int64_t d0 = (int64_t)blockIdx.y * FEW_COLUMNS; d0 < d_end; d0 += 32) {
+    i32x4 h[2][KS];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const int t = k * 32 + grp * 8;
+        h[q][k] = i32x4{0, 0, 0, 0};
+        if (t < t_pad) h[q][k] = *reinterpret_cast<const i32x4*>(ht + min(d0 + q * 16 + i16, D - 1) * t_pad + t);
+      }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          acc[q] = Bf16::mma(h[q][k], hi[p][k], acc[q]);
+          acc[q] = Bf16::mma(h[q][k], lo[p][k], acc[q]);
+        }
+      const int64_t v = v0 + p * 16 + i16;
+      const bool in = v < n;
+      T* row = out + v * stride;
+      if constexpr (sizeof(T) == 2 && !ADD) {
+        uint2 x[2] = {uint2{two_bf16(acc[0][0], acc[0][1]), two_bf16(acc[0][2], acc[0][3])}, uint2{two_bf16(acc[1][0], acc[1][1]), two_bf16(acc[1][2], acc[1][3])}};
+        eight_of(x[0], x[1]);
+        const int64_t d = d0 + 16 * (grp / 2) + 8 * (grp % 2);
+        if (in) put8((uint16_t*)row + d, vec, D - d, uint4{x[0].x, x[0].y, x[1].x, x[1].y});
+      } else {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int64_t d = d0 + q * 16 + grp * 4 + e;
+            if (in && d < D) row[d] = down<T>(ADD ? acc[q][e] + up(row[d]) : acc[q][e]);
+          }
+      }
+    }
   }
 }
 
@@ -544,6 +740,27 @@ Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
   if (weight) {
     L.gt = take(L.rows * L.t16 * 2);
     L.ht = take(D * L.t16 * 2);
+  }
+  return L;
+}
+
+struct FewLayout { int64_t g, gt, ht, sums, total, rows; int t_pad, splits, split_rows; };
+FewLayout few_layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
+  FewLayout L{};
+  auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
+  L.rows = piece_rows(T, V);
+  L.t_pad = (int)(ceil_div(T, 16) * 16);
+  if (hidden) {
+    // enough workgroups to fill the chip, each with at least eight steps
+    const int64_t want = std::min(std::max<int64_t>(1, 1024 / ceil_div(D, 64)), std::max<int64_t>(1, L.rows / (8 * FEW_K)));
+    L.split_rows = (int)(ceil_div(ceil_div(L.rows, want), FEW_K) * FEW_K);
+    L.splits = (int)ceil_div(L.rows, L.split_rows);
+    L.g = take(2 * T * L.rows * 2);
+    L.sums = take((int64_t)L.splits * T * D * 4);
+  }
+  if (weight) {
+    L.gt = take(2 * L.rows * L.t_pad * 2);
+    L.ht = take(D * L.t_pad * 2);
   }
   return L;
 }
@@ -649,7 +866,9 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
 
 extern "C" int64_t simple_xent_grad_workspace(int64_t T, int64_t V, int64_t D, int want_dhidden, int want_dweight) {
   const int rc = check_sizes(T, V, D);
-  return rc != SIMPLE_OK ? rc : layout(T, V, D, want_dhidden != 0, want_dweight != 0).total;
+  if (rc != SIMPLE_OK) return rc;
+  const int64_t all = layout(T, V, D, want_dhidden != 0, want_dweight != 0).total;
+  return T > FEW_GRAD ? all : std::max(all, few_layout(T, V, D, want_dhidden != 0, want_dweight != 0).total);
 }
 
 extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride,
@@ -666,7 +885,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   const Layout L = layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr);
   if (T > 0) {
     if (!dloss_dev || !hidden_dev || !weight_dev || !targets_dev || !lse_dev || !workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
-    if (too_many_tiles(T, V) || workspace_bytes < L.total) return SIMPLE_ECAPACITY;
+    if (too_many_tiles(T, V) || workspace_bytes < simple_xent_grad_workspace(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr)) return SIMPLE_ECAPACITY;
   }
   unsigned char* ws = (unsigned char*)workspace_dev;
   Args a{};
@@ -675,6 +894,65 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   a.scale = logit_scale;
   a.targets = targets_dev;
   a.V = V;
+  a.lse = lse_dev;
+  a.dloss = dloss_dev;
+  const Operand all_rows{(const unsigned char*)weight_dev, weight_stride * 2, V};
+  auto hidden = [&](const float* sums, int splits, const Token* tokens, const uint32_t* top) {
+    auto go = [&](auto kernel, int vec) {
+      const int64_t columns = (int64_t)64 * vec * (splits > 1 ? 1 : HID_GROUPS);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)ceil_div(D, columns)), dim3(64 * HID_GROUPS), 0, st, sums, splits, T, D, tokens, top, targets_dev, dloss_dev, V,
+                         (uint16_t*)dhidden_dev, dhidden_stride);
+    };
+    if (D % 4 == 0 && rows_aligned(dhidden_dev, dhidden_stride, 2, 8)) go(hidden_kernel<4>, 4);
+    else go(hidden_kernel<1>, 1);
+  };
+  if (T > 0 && T <= FEW_GRAD && direct(all_rows, D * 2)) {
+    const FewLayout F = few_layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr);
+    if (dhidden_dev) { a.g = (uint16_t*)(ws + F.g); a.g_stride = F.rows; a.g_plane = T * F.rows; }
+    if (dweight_dev) { a.gt = (uint16_t*)(ws + F.gt); a.gt_stride = F.t_pad; a.gt_plane = F.rows * F.t_pad; }
+    if (dweight_dev)
+      hipLaunchKernelGGL(states_few_kernel, dim3((unsigned)ceil_div(D, 256), (unsigned)(F.t_pad / 8)), dim3(256), 0, st, (const uint16_t*)hidden_dev, hidden_stride, T, D,
+                         F.t_pad, targets_dev, dloss_dev, V, (uint16_t*)(ws + F.ht));
+    for (int64_t v0 = 0; v0 < V; v0 += F.rows) {
+      const int64_t n = std::min(F.rows, V - v0);
+      a.weight = {all_rows.p + v0 * all_rows.stride, all_rows.stride, n};
+      a.v0 = v0;
+      const bool dir = direct(a.hidden, D * 2);
+      auto form = [&](auto shape) {
+        using S = decltype(shape);
+        a.plan = plan<S, false>(T, n);
+        const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
+        if (dir) hipLaunchKernelGGL((g_kernel<S, true, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((g_kernel<S, false, true>), grid, block, 0, st, a);
+      };
+      if (T <= 16) form(Shape<Bf16, 16, 64, 1, 4, 4>{});
+      else if (T <= 32) form(Shape<Bf16, 32, 64, 1, 4, 4>{});
+      else form(Shape<Bf16, 64, 64, 1, 4, 4>{});
+      if (dhidden_dev) {
+        const FewArgs f{a.weight, a.g, a.g_stride, a.g_plane, T, D, F.split_rows, (float*)(ws + F.sums), v0 > 0};
+        const dim3 grid((unsigned)ceil_div(D, 64), (unsigned)F.splits);
+        if (T <= 16) hipLaunchKernelGGL(dh_few_kernel<16>, grid, dim3(256), 0, st, f);
+        else if (T <= 32) hipLaunchKernelGGL(dh_few_kernel<32>, grid, dim3(256), 0, st, f);
+        else hipLaunchKernelGGL(dh_few_kernel<64>, grid, dim3(256), 0, st, f);
+      }
+      if (dweight_dev) {
+        const bool vec = rows_aligned(dweight_dev, dweight_stride, type_bytes(dweight_dtype), 16);
+        auto go = [&](auto kernel, auto* type) {
+          hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(n, 128), (unsigned)ceil_div(D, FEW_COLUMNS)), dim3(256), 0, st, (const uint16_t*)a.gt, a.gt_plane,
+                             (const uint16_t*)(ws + F.ht), F.t_pad, n, D, (decltype(type))dweight_dev + v0 * dweight_stride, dweight_stride, vec);
+        };
+        auto typed = [&](auto ks) {
+          constexpr int KS = decltype(ks)::value;
+          if (dweight_dtype == SIMPLE_F32) { if (accumulate) go(dw_few_kernel<KS, float, true>, (float*)0); else go(dw_few_kernel<KS, float, false>, (float*)0); }
+          else { if (accumulate) go(dw_few_kernel<KS, uint16_t, true>, (uint16_t*)0); else go(dw_few_kernel<KS, uint16_t, false>, (uint16_t*)0); }
+        };
+        if (T <= 32) typed(std::integral_constant<int, 1>{});
+        else typed(std::integral_constant<int, 2>{});
+      }
+    }
+    if (dhidden_dev) hidden((const float*)(ws + F.sums), F.splits, nullptr, nullptr);
+    return launched();
+  }
   uint32_t* tops = (uint32_t*)(ws + L.tops);
   Token* tokens = (Token*)(ws + L.tokens);
   a.tokens = tokens;
@@ -710,8 +988,8 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
         using S = decltype(shape);
         a.plan = plan<S, false>(T, n);
         const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
-        if (dir) hipLaunchKernelGGL((g_kernel<S, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((g_kernel<S, false>), grid, block, 0, st, a);
+        if (dir) hipLaunchKernelGGL((g_kernel<S, true, false>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((g_kernel<S, false, false>), grid, block, 0, st, a);
       });
     }
     if (dhidden_dev) {
@@ -736,14 +1014,6 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       multiply(m, dweight_dtype, accumulate != 0, 1, st);
     }
   }
-  if (dhidden_dev) {
-    auto hidden = [&](auto kernel, int vec) {
-      const int64_t columns = (int64_t)64 * vec * (L.splits > 1 ? 1 : HID_GROUPS);
-      hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)ceil_div(D, columns)), dim3(64 * HID_GROUPS), 0, st, (const float*)(ws + L.sums), L.splits, T, D,
-                         (const Token*)tokens, (const uint32_t*)(tops + TOP_WEIGHTS), (uint16_t*)dhidden_dev, dhidden_stride);
-    };
-    if (D % 4 == 0 && rows_aligned(dhidden_dev, dhidden_stride, 2, 8)) hidden(hidden_kernel<4>, 4);
-    else hidden(hidden_kernel<1>, 1);
-  }
+  if (dhidden_dev) hidden((const float*)(ws + L.sums), L.splits, tokens, tops + TOP_WEIGHTS);
   return launched();
 }

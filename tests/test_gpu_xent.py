@@ -200,3 +200,17 @@ def test_copies_with_aligned_rows_in_more_than_one_piece():
     dh, dw = vocab.linear_xent_grad(dl, h, w, y, lse)
     _check(dh, want["dh"], "dh")
     _check(dw, want["dw"], "dw", BF16)
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_few_tokens_against_more_than_one_piece(T):
+    """A vocabulary of more than 2^20 rows, which is taken in two pieces."""
+    from paper_2512_00719_amd import vocab
+    h, w, y, dl = _inputs(T, 1_100_000, 8, T)
+    y[0] = 1_099_999
+    want = _formula(h, w, y, dl, 1.0)
+    loss, lse = vocab.linear_xent(h, w, y)
+    _check(loss, want["loss"], "loss")
+    dh, dw = vocab.linear_xent_grad(dl, h, w, y, lse)
+    _check(dh, want["dh"], "dh")
+    _check(dw, want["dw"], "dw", BF16)
