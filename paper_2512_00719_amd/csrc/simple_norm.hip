@@ -54,7 +54,8 @@ template <int NT> __device__ __forceinline__ void row_reduce(float& sum, uint32_
   }
 }
 
-// NT threads a row, NV groups of VEC values a thread.
+// NT threads a row, NV groups of VEC values a thread: a row is in registers between its one read and its writes, whatever is computed of it.  Bound:
+// memory; 8192 bfloat16 rows of 4096 with a residual, 268 MB, 44 us (6.1 TB/s, part of it from the caches), 8 rows in 8 bits 5 us (latency).
 template <typename T, int VEC, bool WHOLE, int NT, int NV, int OUT>
 __global__ __launch_bounds__(NT > WG ? NT : WG) void rows_kernel(Args a) {
   constexpr int ROWS = NT > WG ? 1 : WG / NT;
@@ -152,7 +153,8 @@ struct GradArgs {
 };
 
 // A workgroup takes rows a grid apart, so that each of its threads adds up the same columns' weight gradient in registers over all of
-// them; the workgroups' sums are joined by column_sums_kernel in their order.
+// them; the workgroups' sums are joined by column_sums_kernel in their order.  Bound: memory; 8192 bfloat16 rows of 4096 with dh, 268 MB, 46 us, and 5 for
+// joining 1024 workgroups' rows.
 template <typename T, int VEC, bool WHOLE, int NT, int NV>
 __global__ __launch_bounds__(NT > WG ? NT : WG) void grad_kernel(GradArgs a) {
   constexpr int ROWS = NT > WG ? 1 : WG / NT;
