@@ -15,24 +15,26 @@ struct Args {
   Operand tokens, weights;
   int k_bytes, out_type;
   Plan plan;
-  bool vec;             // groups of 16 bytes of the output may be stored together
   const float *scales, *w_scales;
   void* out;
   int64_t out_stride;
 };
 
-template <typename T, bool VEC> __device__ __forceinline__ void put4(T* to, int64_t n, const float (&v)[4]) {
-  if (VEC && n >= 4) store<T, 4>(to, v);
+template <typename T> __device__ __forceinline__ void put4(T* to, int64_t n, const float (&v)[4]) {
+  T x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = down<T>(v[i]);
+  if (n >= 4) __builtin_memcpy(to, x, sizeof(x));  // (any alignment)
   else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (i < n) to[i] = down<T>(v[i]);
+      if (i < n) to[i] = x[i];
   }
 }
 
 template <class S, bool DIRECT> constexpr bool many = DIRECT && Cut<S>::CAN;  // (staged through registers as well, the products' own would spill)
 
-template <class S, bool DIRECT, typename T, bool VEC>
+template <class S, bool DIRECT, typename T>
 __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
   __shared__ __align__(1024) unsigned char lds[S::LDS];
   planned<S, DIRECT, many<S, DIRECT>>(a.tokens, a.weights, a.k_bytes, a.plan, lds, [&](auto shape, auto& acc, int64_t p0, int64_t q0) {
@@ -59,7 +61,7 @@ __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
       const int64_t p = p1 + j * 16;
       const float s = ts[j];
       T* row = (T*)a.out + p * a.out_stride;
-      if constexpr (VEC && sizeof(T) == 2 && R::FQ % 2 == 0) {
+      if constexpr (sizeof(T) == 2 && R::FQ % 2 == 0) {
         const int g = lane >> 4;
         const int64_t q2 = q1 - g * 4 + 16 * (g / 2) + 8 * (g % 2);
 #pragma unroll
@@ -70,7 +72,7 @@ __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
             x[h] = uint2{two_bf16((float)acc[i + h][j][0] * s * ws[i + h][0], (float)acc[i + h][j][1] * s * ws[i + h][1]),
                          two_bf16((float)acc[i + h][j][2] * s * ws[i + h][2], (float)acc[i + h][j][3] * s * ws[i + h][3])};
           eight_of(x[0], x[1]);
-          if (p < a.tokens.rows) put8((uint16_t*)row + q2 + i * 16, true, V - (q2 + i * 16), uint4{x[0].x, x[0].y, x[1].x, x[1].y});
+          if (p < a.tokens.rows) put8((uint16_t*)row + q2 + i * 16, V - (q2 + i * 16), uint4{x[0].x, x[0].y, x[1].x, x[1].y});
         }
       } else {
 #pragma unroll
@@ -78,7 +80,7 @@ __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * s * ws[i][e];
-          if (p < a.tokens.rows) put4<T, VEC>(row + q1 + i * 16, V - (q1 + i * 16), v);
+          if (p < a.tokens.rows) put4<T>(row + q1 + i * 16, V - (q1 + i * 16), v);
         }
       }
     }
@@ -88,13 +90,8 @@ __global__ __launch_bounds__(S::THREADS) void linear_int8_kernel(Args a) {
 template <class S, bool DIRECT> void launch(Args a, hipStream_t st) {
   a.plan = plan<S, many<S, DIRECT>>(a.tokens.rows, a.weights.rows);
   const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
-  if (a.out_type == SIMPLE_F32) {
-    if (a.vec) hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float, false>), grid, block, 0, st, a);
-  } else {
-    if (a.vec) hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, uint16_t, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, uint16_t, false>), grid, block, 0, st, a);
-  }
+  if (a.out_type == SIMPLE_F32) hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, float>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((linear_int8_kernel<S, DIRECT, uint16_t>), grid, block, 0, st, a);
 }
 template <bool DIRECT> void launch_for(const Args& a, hipStream_t st) {
   shaped<Int8>(tiles_for(a.tokens.rows, a.weights.rows), [&](auto shape) { launch<decltype(shape), DIRECT>(a, st); });
@@ -121,8 +118,8 @@ extern "C" int simple_linear_int8(const int8_t* codes_dev, int64_t code_stride, 
   if (workspace_dev && workspace_bytes < simple_linear_int8_workspace(T, V, K)) return SIMPLE_ECAPACITY;
   if (ceil_div(T, 16) * ceil_div(V, 64) > (int64_t)0x7FFFFFFF) return SIMPLE_ECAPACITY;
   const int64_t e = type_bytes(out_dtype);
-  Args a{{(const unsigned char*)codes_dev, code_stride, T}, {(const unsigned char*)w_codes_dev, w_code_stride, V}, (int)K, out_dtype, Plan{},
-         rows_aligned(out_dev, out_stride, e, 16), scales_dev, w_scales_dev, out_dev, out_stride};
+  Args a{{(const unsigned char*)codes_dev, code_stride, T}, {(const unsigned char*)w_codes_dev, w_code_stride, V}, (int)K, out_dtype, Plan{}, scales_dev,
+         w_scales_dev, out_dev, out_stride};
   hipStream_t st = (hipStream_t)hip_stream;
   const Operand weights = a.weights;
   const bool tokens_fit = direct(a.tokens, K), weights_fit = direct(weights, K);

@@ -99,9 +99,10 @@ __device__ __forceinline__ void eight_of(uint2& a, uint2& b) {
   swap(a.y, b.y);
 }
 
-// The first n of eight 16-bit values, together where `to` is 16-byte aligned.
-__device__ __forceinline__ void put8(uint16_t* to, bool aligned, int64_t n, uint4 v) {
-  if (aligned && n >= 8) *reinterpret_cast<uint4*>(to) = v;
+// The first n of eight 16-bit values, to any address of an element (a store of 16 bytes may start anywhere; by single elements dW of 21 tokens with rows of 868
+// took three times as long).
+__device__ __forceinline__ void put8(uint16_t* to, int64_t n, uint4 v) {
+  if (n >= 8) __builtin_memcpy(to, &v, 16);
   else {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll

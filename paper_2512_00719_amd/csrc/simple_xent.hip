@@ -289,7 +289,7 @@ __device__ __forceinline__ void g_of(const Args& a, typename S::Acc (&acc)[S::FQ
   // The second order of a tile that LDS holds whole is made there: two tokens of a column in a word, rows of all the tile's tokens whose 16-byte
   // chunks are stored in an order that spreads a store's eight rows over the banks.  (Stored by single values, it took 25 of a 256 x 256 tile's
   // 130 us; a quarter of the tile at a time, beside the next tile's loads, 6 more than so.)
-  constexpr bool TURN = S::STAGES == 2;
+  constexpr bool TURN = !FEW;
   static_assert(!TURN || S::BP * S::BQ * 2 <= S::LDS, "room");
   constexpr int CHUNKS = S::BP / 8;  // of a row
   auto place = [](int q, int chunk) { return q * (S::BP * 2) + ((chunk ^ ((((q >> 2) & 3) * 2 + (q & 1) * 8) & (CHUNKS - 1))) << 4); };
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
             x[h] = uint2{two_bf16(acc[i + h][j][0] * back, acc[i + h][j][1] * back), two_bf16(acc[i + h][j][2] * back, acc[i + h][j][3] * back)};
           eight_of(x[0], x[1]);
           const int64_t q = q1 + i * 16 + 16 * (g / 2) + 8 * (g % 2);
-          if (in) put8((uint16_t*)row + q, a.vec, a.q.rows - q, uint4{x[0].x, x[0].y, x[1].x, x[1].y});
+          if (in) put8((uint16_t*)row + q, a.q.rows - q, uint4{x[0].x, x[0].y, x[1].x, x[1].y});
         } else {
           const int64_t q = q1 + i * 16 + g * 4;
           float v[4] = {acc[i][j][0] * back, acc[i][j][1] * back, acc[i][j][2] * back, acc[i][j][3] * back};
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(S::THREADS) void mul_kernel(MulArgs a) {
 // take no part.  HID_GROUPS threads share a column group's splits where there are several.
 constexpr int HID_GROUPS = 4;
 template <int VEC>
-__global__ __launch_bounds__(64 * HID_GROUPS) void hidden_kernel(const float* sums, int splits, int64_t T, int64_t D, const Token* tokens, const uint32_t* top,
+__global__ __launch_bounds__(64 * HID_GROUPS) void hidden_kernel(const float* sums, int64_t sums_stride, int splits, int64_t T, int64_t D, const Token* tokens, const uint32_t* top,
                                                                  const int32_t* targets, const float* dloss, int64_t V, uint16_t* out, int64_t stride) {
   __shared__ float part[HID_GROUPS][64 * VEC];
   const int64_t t = blockIdx.x;
@@ -506,11 +506,11 @@ __global__ __launch_bounds__(64 * HID_GROUPS) void hidden_kernel(const float* su
 #pragma unroll
   for (int e = 0; e < VEC; ++e) v[e] = 0.f;
   if (c < D && on) {
-    const float* p = sums + t * D + c;
+    const float* p = sums + t * sums_stride + c;
 #pragma unroll 8
     for (int s = shared_out ? grp : 0; s < splits; s += HID_GROUPS) {
       float x[VEC];
-      load<float, VEC>(p + (int64_t)s * T * D, x);
+      load<float, VEC>(p + (int64_t)s * T * sums_stride, x);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) v[e] += x[e];
     }
@@ -550,7 +550,7 @@ __device__ __forceinline__ i32x4 turned(const unsigned char* rows0, const unsign
 struct FewArgs {
   Operand weight;          // the piece's rows
   const uint16_t* g;       // two planes [T][g_stride]
-  int64_t g_stride, g_plane, T, D;
+  int64_t g_stride, g_plane, T, D;  // D: a multiple of 8, the weights' rows have as many values
   int split_rows;          // of the weights, a multiple of FEW_K
   float* sums;             // [splits][T][D]
   int add;
@@ -613,7 +613,7 @@ __global__ __launch_bounds__(256) void dh_few_kernel(FewArgs a) {
 #pragma unroll
   for (int j = 0; j < FP; ++j) {
     const int64_t t = j * 16 + i16, d = d0 + wave * 16 + grp * 4;
-    if (t >= a.T || d >= a.D) continue;  // (D is a multiple of 8)
+    if (t >= a.T || d >= a.D) continue;
     float* to = a.sums + ((int64_t)blockIdx.y * a.T + t) * a.D + d;
     float v[4] = {acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
     if (a.add) {
@@ -638,18 +638,17 @@ __global__ __launch_bounds__(256) void states_few_kernel(const uint16_t* h, int6
   *reinterpret_cast<Group<uint16_t, 8>*>(out + d * t_pad + t0) = v;
 }
 
-// dW[v][d] (+)= sum over the tokens of G[t][v] H[t][d]: a wave has 32 rows v, whose fragments stay in registers, against the columns d in turn, 32 at a time.  Nothing goes
+// dW[v][d] (+)= sum over the tokens of G[t][v] H[t][d]: a wave has 16 FEW_V rows v, whose fragments stay in registers, against the columns d in turn, 32 at a time.  Nothing goes
 // through LDS: the states, [D][t_pad], come from the caches.  Bound: one write of the gradient.
-constexpr int FEW_COLUMNS = 256;
+constexpr int FEW_COLUMNS = 256, FEW_V = 4;
 template <int KS, typename T, bool ADD>
-__global__ __launch_bounds__(256) void dw_few_kernel(const uint16_t* gt, int64_t plane, const uint16_t* ht, int t_pad, int64_t n, int64_t D, T* out, int64_t stride,
-                                                     bool vec) {
+__global__ __launch_bounds__(256) void dw_few_kernel(const uint16_t* gt, int64_t plane, const uint16_t* ht, int t_pad, int64_t n, int64_t D, T* out, int64_t stride) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, grp = lane >> 4;
-  const int64_t v0 = ((int64_t)blockIdx.x * 4 + wave) * 32;
+  const int64_t v0 = ((int64_t)blockIdx.x * 4 + wave) * (16 * FEW_V);
   if (v0 >= n) return;
-  i32x4 hi[2][KS], lo[2][KS];
+  i32x4 hi[FEW_V][KS], lo[FEW_V][KS];
 #pragma unroll
-  for (int p = 0; p < 2; ++p)
+  for (int p = 0; p < FEW_V; ++p)
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       const int t = k * 32 + grp * 8;
@@ -673,7 +672,7 @@ __global__ __launch_bounds__(256) void dw_few_kernel(const uint16_t* gt, int64_t
         if (t < t_pad) h[q][k] = *reinterpret_cast<const i32x4*>(ht + min(d0 + q * 16 + i16, D - 1) * t_pad + t);
       }
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
+    for (int p = 0; p < FEW_V; ++p) {
       f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int q = 0; q < 2; ++q)
@@ -689,7 +688,7 @@ __global__ __launch_bounds__(256) void dw_few_kernel(const uint16_t* gt, int64_t
         uint2 x[2] = {uint2{two_bf16(acc[0][0], acc[0][1]), two_bf16(acc[0][2], acc[0][3])}, uint2{two_bf16(acc[1][0], acc[1][1]), two_bf16(acc[1][2], acc[1][3])}};
         eight_of(x[0], x[1]);
         const int64_t d = d0 + 16 * (grp / 2) + 8 * (grp % 2);
-        if (in) put8((uint16_t*)row + d, vec, D - d, uint4{x[0].x, x[0].y, x[1].x, x[1].y});
+        if (in) put8((uint16_t*)row + d, D - d, uint4{x[0].x, x[0].y, x[1].x, x[1].y});
       } else {
 #pragma unroll
         for (int q = 0; q < 2; ++q)
@@ -713,8 +712,7 @@ int64_t piece_rows(int64_t T, int64_t V) {
 }
 // Workgroups a tile of dH: enough to fill the chip, each with at least 16 steps of k.
 int hidden_splits(int64_t T, int64_t V, int64_t D) {
-  const int64_t bp = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : 256;
-  const int64_t tiles = std::max<int64_t>(1, ceil_div(T, bp) * ceil_div(D, T <= 64 ? 64 : T <= 128 ? 128 : 256)), want = T <= 64 ? 1024 : T <= 128 ? 512 : 256;
+  const int64_t side = T <= 128 ? 128 : 256, tiles = std::max<int64_t>(1, ceil_div(T, side) * ceil_div(D, side)), want = T <= 128 ? 512 : 256;
   const int64_t most = std::max<int64_t>(1, piece_rows(T, V) * 2 / (16 * KB));
   return (int)std::max<int64_t>(1, std::min(most, want / tiles));
 }
@@ -746,19 +744,24 @@ Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
   return L;
 }
 
-struct FewLayout { int64_t g, gt, ht, sums, total, rows; int t_pad, splits, split_rows; };
-FewLayout few_layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
+struct FewLayout { int64_t copy_h, copy_w, g, gt, ht, sums, total, rows, d_pad; int t_pad, splits, split_rows; };
+FewLayout few_layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight, bool copies) {
   FewLayout L{};
   auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
-  L.rows = piece_rows(T, V);
+  L.rows = copies ? std::min(ALIGN_ROWS, ceil_div(V, ROUND) * ROUND) : piece_rows(T, V);
   L.t_pad = (int)(ceil_div(T, 16) * 16);
+  L.d_pad = ceil_div(D, 8) * 8;
+  if (copies) {
+    L.copy_h = take(T * L.d_pad * 2);
+    L.copy_w = take(L.rows * L.d_pad * 2);
+  }
   if (hidden) {
     // enough workgroups to fill the chip, each with at least eight steps
     const int64_t want = std::min(std::max<int64_t>(1, 1024 / ceil_div(D, 64)), std::max<int64_t>(1, L.rows / (8 * FEW_K)));
     L.split_rows = (int)(ceil_div(ceil_div(L.rows, want), FEW_K) * FEW_K);
     L.splits = (int)ceil_div(L.rows, L.split_rows);
     L.g = take(2 * T * L.rows * 2);
-    L.sums = take((int64_t)L.splits * T * D * 4);
+    L.sums = take((int64_t)L.splits * T * L.d_pad * 4);
   }
   if (weight) {
     L.gt = take(2 * L.rows * L.t_pad * 2);
@@ -869,8 +872,8 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
 extern "C" int64_t simple_xent_grad_workspace(int64_t T, int64_t V, int64_t D, int want_dhidden, int want_dweight) {
   const int rc = check_sizes(T, V, D);
   if (rc != SIMPLE_OK) return rc;
-  const int64_t all = layout(T, V, D, want_dhidden != 0, want_dweight != 0).total;
-  return T > FEW_GRAD ? all : std::max(all, few_layout(T, V, D, want_dhidden != 0, want_dweight != 0).total);
+  const bool h = want_dhidden != 0, w = want_dweight != 0;
+  return T > FEW_GRAD || T == 0 ? layout(T, V, D, h, w).total : std::max(few_layout(T, V, D, h, w, false).total, few_layout(T, V, D, h, w, true).total);
 }
 
 extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride,
@@ -899,17 +902,20 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   a.lse = lse_dev;
   a.dloss = dloss_dev;
   const Operand all_rows{(const unsigned char*)weight_dev, weight_stride * 2, V};
-  auto hidden = [&](const float* sums, int splits, const Token* tokens, const uint32_t* top) {
+  auto hidden = [&](const float* sums, int64_t sums_stride, int splits, const Token* tokens, const uint32_t* top) {
     auto go = [&](auto kernel, int vec) {
       const int64_t columns = (int64_t)64 * vec * (splits > 1 ? 1 : HID_GROUPS);
-      hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)ceil_div(D, columns)), dim3(64 * HID_GROUPS), 0, st, sums, splits, T, D, tokens, top, targets_dev, dloss_dev, V,
+      hipLaunchKernelGGL(kernel, dim3((unsigned)T, (unsigned)ceil_div(D, columns)), dim3(64 * HID_GROUPS), 0, st, sums, sums_stride, splits, T, D, tokens, top, targets_dev, dloss_dev, V,
                          (uint16_t*)dhidden_dev, dhidden_stride);
     };
-    if (D % 4 == 0 && rows_aligned(dhidden_dev, dhidden_stride, 2, 8)) go(hidden_kernel<4>, 4);
+    if (D % 4 == 0 && sums_stride % 4 == 0 && rows_aligned(dhidden_dev, dhidden_stride, 2, 8)) go(hidden_kernel<4>, 4);
     else go(hidden_kernel<1>, 1);
   };
-  if (T > 0 && T <= FEW_GRAD && direct(all_rows, D * 2)) {
-    const FewLayout F = few_layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr);
+  if (T > 0 && T <= FEW_GRAD) {
+    const bool fits = direct(a.hidden, D * 2) && direct(all_rows, D * 2);  // else copies with aligned rows, of the weights a piece at a time
+    const FewLayout F = few_layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr, !fits);
+    a.k_bytes = (int)(F.d_pad * 2);
+    if (!fits) a.hidden = aligned_copy<2>(a.hidden, D * 2, ws + F.copy_h, st);
     if (dhidden_dev) { a.g = (uint16_t*)(ws + F.g); a.g_stride = F.rows; a.g_plane = T * F.rows; }
     if (dweight_dev) { a.gt = (uint16_t*)(ws + F.gt); a.gt_stride = F.t_pad; a.gt_plane = F.rows * F.t_pad; }
     if (dweight_dev)
@@ -919,29 +925,26 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       const int64_t n = std::min(F.rows, V - v0);
       a.weight = {all_rows.p + v0 * all_rows.stride, all_rows.stride, n};
       a.v0 = v0;
-      const bool dir = direct(a.hidden, D * 2);
+      if (!fits) a.weight = aligned_copy<2>(a.weight, D * 2, ws + F.copy_w, st);
       auto form = [&](auto shape) {
         using S = decltype(shape);
         a.plan = plan<S, false>(T, n);
-        const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
-        if (dir) hipLaunchKernelGGL((g_kernel<S, true, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((g_kernel<S, false, true>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((g_kernel<S, true, true>), dim3((unsigned)a.plan.grid), dim3(S::THREADS), 0, st, a);
       };
       if (T <= 16) form(Shape<Bf16, 16, 64, 1, 4, 4>{});
       else if (T <= 32) form(Shape<Bf16, 32, 64, 1, 4, 4>{});
       else form(Shape<Bf16, 64, 64, 1, 4, 4>{});
       if (dhidden_dev) {
-        const FewArgs f{a.weight, a.g, a.g_stride, a.g_plane, T, D, F.split_rows, (float*)(ws + F.sums), v0 > 0};
+        const FewArgs f{a.weight, a.g, a.g_stride, a.g_plane, T, F.d_pad, F.split_rows, (float*)(ws + F.sums), v0 > 0};
         const dim3 grid((unsigned)ceil_div(D, 64), (unsigned)F.splits);
         if (T <= 16) hipLaunchKernelGGL(dh_few_kernel<16>, grid, dim3(256), 0, st, f);
         else if (T <= 32) hipLaunchKernelGGL(dh_few_kernel<32>, grid, dim3(256), 0, st, f);
         else hipLaunchKernelGGL(dh_few_kernel<64>, grid, dim3(256), 0, st, f);
       }
       if (dweight_dev) {
-        const bool vec = rows_aligned(dweight_dev, dweight_stride, type_bytes(dweight_dtype), 16);
         auto go = [&](auto kernel, auto* type) {
-          hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(n, 128), (unsigned)ceil_div(D, FEW_COLUMNS)), dim3(256), 0, st, (const uint16_t*)a.gt, a.gt_plane,
-                             (const uint16_t*)(ws + F.ht), F.t_pad, n, D, (decltype(type))dweight_dev + v0 * dweight_stride, dweight_stride, vec);
+          hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(n, 64 * FEW_V), (unsigned)ceil_div(D, FEW_COLUMNS)), dim3(256), 0, st, (const uint16_t*)a.gt, a.gt_plane,
+                             (const uint16_t*)(ws + F.ht), F.t_pad, n, D, (decltype(type))dweight_dev + v0 * dweight_stride, dweight_stride);
         };
         auto typed = [&](auto ks) {
           constexpr int KS = decltype(ks)::value;
@@ -952,7 +955,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
         else typed(std::integral_constant<int, 2>{});
       }
     }
-    if (dhidden_dev) hidden((const float*)(ws + F.sums), F.splits, nullptr, nullptr);
+    if (dhidden_dev) hidden((const float*)(ws + F.sums), F.d_pad, F.splits, nullptr, nullptr);
     return launched();
   }
   uint32_t* tops = (uint32_t*)(ws + L.tops);
@@ -986,13 +989,15 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
     if (copies) a.weight = aligned_copy<2>(a.weight, D * 2, ws + L.copy_w, st);
     if (T > 0) {
       const bool dir = direct(a.hidden, a.k_bytes) && direct(a.weight, a.k_bytes);
-      shaped<Bf16>(tiles_for(T, n), [&](auto shape) {
+      auto form = [&](auto shape) {
         using S = decltype(shape);
         a.plan = plan<S, false>(T, n);
         const dim3 grid((unsigned)a.plan.grid), block(S::THREADS);
         if (dir) hipLaunchKernelGGL((g_kernel<S, true, false>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((g_kernel<S, false, false>), grid, block, 0, st, a);
-      });
+      };
+      if (tiles_for(T, n) == TILE_256) form(Shape<Bf16, 256, 256, 2, 4, 2>{});
+      else form(Shape<Bf16, 128, 128, 2, 2, 2>{});
     }
     if (dhidden_dev) {
       transpose((const uint16_t*)a.weight.p, a.weight.stride / 2, n, D, (uint16_t*)(ws + L.wt), L.rows, n8, nullptr, tops + TOP_WEIGHTS, st);
@@ -1016,6 +1021,6 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       multiply(m, dweight_dtype, accumulate != 0, 1, st);
     }
   }
-  if (dhidden_dev) hidden((const float*)(ws + L.sums), L.splits, tokens, tops + TOP_WEIGHTS);
+  if (dhidden_dev) hidden((const float*)(ws + L.sums), D, L.splits, tokens, tops + TOP_WEIGHTS);
   return launched();
 }
