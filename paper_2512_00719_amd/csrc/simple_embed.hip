@@ -175,6 +175,7 @@ __global__ __launch_bounds__(WG) void place_kernel(Sort s, Fill f) {
   static_assert(2 * WG >= BINS, "two digits a thread");
   const int tid = threadIdx.x;
   int32_t ahead[2] = {0, 0}, all[2] = {0, 0};  // counts of the tiles ahead, and of all
+  // (Each tile counting all of them itself would spare a kernel a pass: 16,384 tokens 125 us so, 117 with the counts of the kernel before.)
 #pragma unroll 4
   for (int t = 0; t < s.tiles; ++t) {
     const int2 c = *reinterpret_cast<const int2*>(s.counts + (int64_t)t * BINS + 2 * tid);
@@ -342,6 +343,57 @@ __global__ __launch_bounds__(WG) void join_kernel(Sums s) {
   finish<TO, VEC>(s, id, c, acc);
 }
 
+// Up to DIRECT tokens need no sort: the workgroup of an id's first token finds the others and sums them in their order, CHUNK at a time as the sums above do.
+// One kernel where five steps of 3 to 5 us each would wait for each other (219 tokens into 87,057 x 89 float32, zeros and all: 26 us sorted, 14 so).
+constexpr int DIRECT = 256;
+template <typename T, typename TO, int VEC>
+__global__ __launch_bounds__(WG) void direct_kernel(Sums s, const int32_t* ids) {
+  __shared__ int32_t id[DIRECT], same[DIRECT];
+  __shared__ int found;
+  const int t = blockIdx.x, n = (int)s.n;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) id[i] = ids[i];
+  __syncthreads();
+  const int32_t own = id[t];
+  if (own < 0 || own >= s.V) return;
+  if (threadIdx.x < 64) {  // places of the id's tokens, in order; none if this is not its first
+    int m = 0;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+      const int i = i0 + threadIdx.x;
+      const bool is = i < n && id[i] == own;
+      const uint64_t all = __ballot(is);
+      if (m == 0 && all != 0 && i0 + __ffsll((unsigned long long)all) - 1 != t) break;
+      if (is) same[m + (int)__popcll(all & ((1ull << threadIdx.x) - 1ull))] = i;
+      m += (int)__popcll(all);
+    }
+    if (threadIdx.x == 0) found = m;
+  }
+  __syncthreads();
+  const int m = found;
+  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+  if (m == 0 || c >= s.D) return;
+  const T* d = (const T*)s.dout + c;
+  constexpr int AHEAD = 8;
+  float sum[VEC], acc[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] = acc[j] = 0.f;
+  for (int i0 = 0; i0 < m; i0 += AHEAD) {
+    float v[AHEAD][VEC];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) load<T, VEC>(d + same[min(i0 + u, m - 1)] * s.dout_stride, v[u]);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (i0 + u < m) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
+      }
+    if ((i0 + AHEAD) % CHUNK == 0 || i0 + AHEAD >= m) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) { sum[j] += acc[j]; acc[j] = 0.f; }
+    }
+  }
+  finish<TO, VEC>(s, own, c, sum);
+}
+
 struct Layout { int64_t key[2], pos[2], counts, partial, total; int tiles, passes; };
 Layout layout(int64_t T, int64_t V, int64_t D) {
   Layout L{};
@@ -418,9 +470,14 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
   const int64_t eo = type_bytes(table_dtype), ei = type_bytes(dtype);
   Sort s{ids_dev, nullptr, (int32_t*)(ws + L.key[0]), (int32_t*)(ws + L.pos[0]), (int32_t*)(ws + L.counts), T, V, L.tiles, 0};
   Fill zeros{(unsigned char*)dtable_dev, V, D * eo, dtable_stride * eo, 0};
-  if (T <= FEW) {
+  if (T <= DIRECT) {
+    if (!accumulate) {
+      s.n = 0;  // (zeros alone)
+      hipLaunchKernelGGL(sort_few_kernel, dim3((unsigned)fill_workgroups(zeros, FEW_WG)), dim3(FEW_WG), 0, st, s, 0, zeros);
+    }
+  } else if (T <= FEW) {
     const int64_t shares = accumulate ? 0 : fill_workgroups(zeros, FEW_WG);
-    hipLaunchKernelGGL(sort_few_kernel, dim3((unsigned)(shares + (T > 0))), dim3(FEW_WG), 0, st, s, L.passes, zeros);
+    hipLaunchKernelGGL(sort_few_kernel, dim3((unsigned)(shares + 1)), dim3(FEW_WG), 0, st, s, L.passes, zeros);
     s.key_in = s.key_out; s.pos_in = s.pos_out;
   } else {
     const int kernels = 2 * L.passes;
@@ -450,18 +507,22 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
   const int x = std::max(64, shape_of(units));
   const dim3 grid((unsigned)chunks, (unsigned)ceil_div(units, x)), rest((unsigned)(chunks - 1), grid.y);
   if (grid.y > 65535) return SIMPLE_ECAPACITY;
-  auto go = [&](auto sums, auto join) {
+  auto go = [&](auto direct, auto sums, auto join) {
+    if (T <= DIRECT) {
+      hipLaunchKernelGGL(direct, dim3((unsigned)T, grid.y), dim3(x), 0, st, m, ids_dev);
+      return;
+    }
     hipLaunchKernelGGL(sums, grid, dim3(x), 0, st, m);
-    if (chunks > 1) hipLaunchKernelGGL(join, rest, dim3(x), 0, st, m);
+    hipLaunchKernelGGL(join, rest, dim3(x), 0, st, m);  // (more than DIRECT tokens are more than one chunk)
   };
   if (dtype == SIMPLE_BF16 && table_dtype == SIMPLE_BF16) {
-    if (wide) go(sums_kernel<uint16_t, uint16_t, 8>, join_kernel<uint16_t, 8>); else go(sums_kernel<uint16_t, uint16_t, 1>, join_kernel<uint16_t, 1>);
+    if (wide) go(direct_kernel<uint16_t, uint16_t, 8>, sums_kernel<uint16_t, uint16_t, 8>, join_kernel<uint16_t, 8>); else go(direct_kernel<uint16_t, uint16_t, 1>, sums_kernel<uint16_t, uint16_t, 1>, join_kernel<uint16_t, 1>);
   } else if (dtype == SIMPLE_BF16) {
-    if (wide) go(sums_kernel<uint16_t, float, 4>, join_kernel<float, 4>); else go(sums_kernel<uint16_t, float, 1>, join_kernel<float, 1>);
+    if (wide) go(direct_kernel<uint16_t, float, 4>, sums_kernel<uint16_t, float, 4>, join_kernel<float, 4>); else go(direct_kernel<uint16_t, float, 1>, sums_kernel<uint16_t, float, 1>, join_kernel<float, 1>);
   } else if (table_dtype == SIMPLE_BF16) {
-    if (wide) go(sums_kernel<float, uint16_t, 4>, join_kernel<uint16_t, 4>); else go(sums_kernel<float, uint16_t, 1>, join_kernel<uint16_t, 1>);
+    if (wide) go(direct_kernel<float, uint16_t, 4>, sums_kernel<float, uint16_t, 4>, join_kernel<uint16_t, 4>); else go(direct_kernel<float, uint16_t, 1>, sums_kernel<float, uint16_t, 1>, join_kernel<uint16_t, 1>);
   } else {
-    if (wide) go(sums_kernel<float, float, 4>, join_kernel<float, 4>); else go(sums_kernel<float, float, 1>, join_kernel<float, 1>);
+    if (wide) go(direct_kernel<float, float, 4>, sums_kernel<float, float, 4>, join_kernel<float, 4>); else go(direct_kernel<float, float, 1>, sums_kernel<float, float, 1>, join_kernel<float, 1>);
   }
   return launched();
 }

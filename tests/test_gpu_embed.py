@@ -44,7 +44,7 @@ def test_lookup(T, V, D, pad, shift, dtype):
 @pytest.mark.parametrize("types", [(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)])
 @pytest.mark.parametrize("kind", ["uniform", "skewed", "one", "runs", "invalid", "nothing"])
 @pytest.mark.parametrize("T,V,D", [(1, 1, 1), (31, 40, 7), (32, 600, 64), (33, 513, 65), (2047, 3000, 40), (2049, 511, 24), (4100, 262_143, 8), (9000, 512, 136),
-                                   (700, 50, 2064)])
+                                   (700, 50, 2064), (200, 90, 130), (256, 1000, 72), (257, 1000, 72), (16_384, 300, 16), (17_000, 70_000, 16)])
 def test_gradient(T, V, D, kind, types):
     """A token's term passes through its chunk's 32 additions and those of the chunks behind it: T / 32 + 32 roundings of 2^-24 on the sum of
     the terms' magnitudes, then the scale's and, added to what was there, one more of float32 and that of the output's type."""
