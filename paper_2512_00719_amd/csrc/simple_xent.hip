@@ -933,7 +933,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
       };
       if (T <= 16) form(Shape<Bf16, 16, 64, 1, 4, 4>{});
       else if (T <= 32) form(Shape<Bf16, 32, 64, 1, 4, 4>{});
-      else form(Shape<Bf16, 64, 64, 1, 4, 4>{});
+      else form(Shape<Bf16, 64, 128, 1, 4, 3>{});
       if (dhidden_dev) {
         const FewArgs f{a.weight, a.g, a.g_stride, a.g_plane, T, F.d_pad, F.split_rows, (float*)(ws + F.sums), v0 > 0};
         const dim3 grid((unsigned)ceil_div(D, 64), (unsigned)F.splits);
