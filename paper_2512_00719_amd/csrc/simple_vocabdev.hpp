@@ -100,10 +100,13 @@ __device__ __forceinline__ void eight_of(uint2& a, uint2& b) {
 }
 
 // The first n of eight 16-bit values, to any address of an element (a store of 16 bytes may start anywhere; by single elements dW of 21 tokens with rows of 868
-// took three times as long).
-__device__ __forceinline__ void put8(uint16_t* to, int64_t n, uint4 v) {
-  if (n >= 8) __builtin_memcpy(to, &v, 16);
-  else {
+// took three times as long).  PAST: the caches are not to keep them.
+template <bool PAST = false> __device__ __forceinline__ void put8(uint16_t* to, int64_t n, uint4 v) {
+  if (n >= 8) {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    if constexpr (PAST) __builtin_nontemporal_store(words{v.x, v.y, v.z, v.w}, reinterpret_cast<words*>(to));
+    else __builtin_memcpy(to, &v, 16);
+  } else {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
