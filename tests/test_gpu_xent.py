@@ -100,6 +100,28 @@ def test_strides_and_alignments(T, V, D, pad, shift):
     assert padding_untouched(dh, pad, shift) and padding_untouched(dw, pad, shift)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("pad,shift", [(24, 0), (24, 8), (1, 3)])
+@pytest.mark.parametrize("T,D", [(5, 40), (50, 104)])
+def test_few_tokens_weight_gradient_added_in_place(T, D, pad, shift, dtype):
+    """Rows of whole 64 bytes (pad 24) with a short last piece, and others: the sum with zeros is the gradient bit for bit, padding stays."""
+    from paper_2512_00719_amd import vocab
+    V = 333
+    h, w, y, dl = _inputs(T, V, D, 8)
+    want = _formula(h, w, y, dl, 1.0)
+    lse = vocab.linear_xent(h, w, y)[1]
+    plain, added, twice = (laid(torch.zeros(V, D, dtype=dtype, device=DEV), pad, shift) for _ in range(3))
+    vocab.linear_xent_grad(dl, h, w, y, lse, dweight=plain, need_dhidden=False)
+    _check(plain, want["dw"], "dw", dtype)
+    vocab.linear_xent_grad(dl, h, w, y, lse, dweight=added, accumulate=True, need_dhidden=False)
+    assert torch.equal(added, plain)
+    twice.fill_(1.0)
+    vocab.linear_xent_grad(dl, h, w, y, lse, dweight=twice, accumulate=True, need_dhidden=False)
+    value, off = want["dw"]
+    within(twice, value + 1.0, off + (value + 1.0).abs() * HALF[dtype] + 1e-30, "dw")
+    assert all(padding_untouched(t, pad, shift) for t in (plain, added, twice))
+
+
 def test_pieces_of_the_vocabulary():
     """More than one piece, the last of them short: 40,000 tokens have pieces of 4096 rows."""
     from paper_2512_00719_amd import vocab
