@@ -21,6 +21,7 @@ constexpr int RD = 4;              // rows in flight per thread of the lookup
 constexpr int TILE = 1024;         // tokens a workgroup of the sort
 constexpr int BITS = 9, BINS = 1 << BITS;
 constexpr int CHUNK = 32;          // sorted places a workgroup of the sums
+constexpr int FEW_CHUNK = 16;      // the same of up to FEW tokens, whose sums wait for one workgroup's rows (600 tokens of 1024 values: 9.6 us, 16.7 with 32)
 constexpr int ROUNDS = TILE / WG;  // a wave's tokens, 64 at a time
 
 // ---- lookup ----
@@ -242,41 +243,42 @@ struct Sums {
   float scale;
   void* dtable;
   int64_t dtable_stride;
-  int accumulate;
+  int chunk;       // sorted places a workgroup of the sums
   float* partial;  // [chunks][2][D]: of the row that the chunk begins inside, and of the one that it ends inside
 };
 
-template <typename TO, int VEC> __device__ __forceinline__ void finish(const Sums& s, int32_t id, int64_t c, float (&acc)[VEC]) {
-  TO* to = (TO*)s.dtable + id * s.dtable_stride + c;
+template <typename TO, int VEC, bool WHOLE, bool ADD> __device__ __forceinline__ void finish(const Sums& s, int32_t id, int64_t c, float (&acc)[VEC]) {
+  TO* row = (TO*)s.dtable + id * s.dtable_stride;
   float v[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) v[j] = 0.f;
-  if (s.accumulate) load<TO, VEC>(to, v);
+  if constexpr (ADD) load_some<TO, VEC, WHOLE>(row, c, s.D, v);
 #pragma unroll
   for (int j = 0; j < VEC; ++j) v[j] = fmaf(acc[j], s.scale, v[j]);
-  store<TO, VEC>(to, v);
+  store_some<TO, VEC, WHOLE>(row + c, s.D - c, v);
 }
 
-template <typename T, typename TO, int VEC>
+template <typename T, typename TO, int VEC, bool ADD>
 __global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
   __shared__ int32_t key[CHUNK + 2], pos[CHUNK];
-  const int64_t chunk = blockIdx.x, s0 = chunk * CHUNK;
-  const int m = (int)min((int64_t)CHUNK, s.n - s0);
-  for (int i = threadIdx.x; i < CHUNK + 2; i += blockDim.x) {
+  const int64_t chunk = blockIdx.x, s0 = chunk * s.chunk;
+  int m = (int)min((int64_t)s.chunk, s.n - s0);
+  for (int i = threadIdx.x; i < s.chunk + 2; i += blockDim.x) {
     const int64_t at = s0 + i - 1;
     key[i] = at >= 0 && at < s.n ? s.key[at] : -1;
-    if (i < CHUNK) pos[i] = s.pos[s0 + (i < m ? i : 0)];
+    if (i < s.chunk) pos[i] = s.pos[s0 + (i < m ? i : 0)];
   }
   __syncthreads();
   const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
-  if (c >= s.D || key[1] >= s.V) return;
+  while (m > 0 && key[m] >= s.V) --m;  // (tokens outside the vocabulary are sorted behind the others)
+  if (c >= s.D || m == 0) return;
   const T* d = (const T*)s.dout + c;
   float acc[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
   bool inside = key[0] == key[1];  // the row began in an earlier chunk
   constexpr int AHEAD = 8;
-  static_assert(CHUNK % AHEAD == 0, "loads in flight");
+  static_assert(CHUNK % AHEAD == 0 && FEW_CHUNK % AHEAD == 0, "loads in flight");
   for (int i0 = 0; i0 < m; i0 += AHEAD) {
     float v[AHEAD][VEC];
 #pragma unroll
@@ -284,37 +286,35 @@ __global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int i = i0 + u;
-      if (i >= m || key[1 + i] >= s.V) return;
+      if (i >= m) break;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
-      if (key[1 + i] != key[2 + i]) {  // the row's last token
-        if (inside) store<float, VEC>(s.partial + 2 * chunk * s.D + c, acc);
-        else finish<TO, VEC>(s, key[1 + i], c, acc);
+      const bool last = key[1 + i] != key[2 + i];  // the row's last token
+      if (!last && i < m - 1) continue;
+      if (last && !inside) finish<TO, VEC, true, ADD>(s, key[1 + i], c, acc);
+      else store<float, VEC>(s.partial + (2 * chunk + (inside ? 0 : 1)) * s.D + c, acc);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
-        inside = false;
-      } else if (i == m - 1) {         // the row runs on
-        store<float, VEC>(s.partial + (2 * chunk + (inside ? 0 : 1)) * s.D + c, acc);
-      }
+      for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
+      inside = false;
     }
   }
 }
 
 // The row that chunk blockIdx.x ends inside, if it began there: its partial sums, in order.  12 us where the most frequent of 16,384 tokens has 1300 of them, 41
 // chunks; eight partial rows in flight.
-template <typename TO, int VEC>
+template <typename TO, int VEC, bool ADD>
 __global__ __launch_bounds__(WG) void join_kernel(Sums s) {
-  const int64_t chunk = blockIdx.x, e = (chunk + 1) * CHUNK;  // (the grid leaves the last chunk out)
+  const int64_t chunk = blockIdx.x, e = (chunk + 1) * s.chunk;  // (the grid leaves the last chunk out)
   const int32_t id = s.key[e - 1];
   if (id >= s.V || s.key[e] != id) return;
-  if (s.key[chunk * CHUNK] == id && chunk > 0 && s.key[chunk * CHUNK - 1] == id) return;
+  if (s.key[chunk * s.chunk] == id && chunk > 0 && s.key[chunk * s.chunk - 1] == id) return;
   // the first chunk that the row does not run out of
   __shared__ int32_t found;
   int64_t end = chunk + 1;
   for (bool more = true; more; ) {
     if (threadIdx.x == 0) found = (int32_t)blockDim.x;
     __syncthreads();
-    const int64_t after = (end + threadIdx.x + 1) * CHUNK;  // the place behind chunk end + threadIdx.x
+    const int64_t after = (end + threadIdx.x + 1) * s.chunk;  // the place behind chunk end + threadIdx.x
     if (after >= s.n || s.key[after] != id) atomicMin(&found, (int32_t)threadIdx.x);
     __syncthreads();
     end += found;
@@ -340,61 +340,79 @@ __global__ __launch_bounds__(WG) void join_kernel(Sums s) {
         for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
       }
   }
-  finish<TO, VEC>(s, id, c, acc);
+  finish<TO, VEC, true, ADD>(s, id, c, acc);
 }
 
-// Up to DIRECT tokens need no sort: the workgroup of an id's first token finds the others and sums them in their order, CHUNK at a time as the sums above do.
-// One kernel where five steps of 3 to 5 us each would wait for each other (219 tokens into 87,057 x 89 float32, zeros and all: 26 us sorted, 14 so).
-constexpr int DIRECT = 256;
-template <typename T, typename TO, int VEC>
-__global__ __launch_bounds__(WG) void direct_kernel(Sums s, const int32_t* ids) {
+// Up to DIRECT tokens need no sort: the workgroup of an id's first token finds the others and sums them in their order, CHUNK at a time, chunks in turn by the groups of
+// `blockDim.x` threads, whose sums are joined in the groups' order.  One kernel where five steps of 3 to 5 us each would wait for each other (a call with 219 tokens of
+// 89 values float32 26 us sorted, 14 so; 300 and 512 of 1024 bfloat16 33 and 15).  Every token has its workgroups: no more than DIRECT_WGS, two rounds of the chip
+// (512 tokens of 7172 values, 4096 workgroups: 28 us sorted, 36 so).  600 tokens of 1024 values took 18 us this way, but 46 with one id in most of them, 28 sorted.
+constexpr int DIRECT = 512, DIRECT_WG = 512;
+constexpr int64_t DIRECT_WGS = 2048;
+template <typename T, typename TO, int VEC, bool WHOLE, bool ADD>
+__global__ __launch_bounds__(DIRECT_WG) void direct_kernel(Sums s, const int32_t* ids) {
   __shared__ int32_t id[DIRECT], same[DIRECT];
   __shared__ int found;
-  const int t = blockIdx.x, n = (int)s.n;
-  for (int i = threadIdx.x; i < n; i += blockDim.x) id[i] = ids[i];
+  __shared__ float others[DIRECT_WG * VEC];
+  const int t = blockIdx.x, n = (int)s.n, thread = threadIdx.y * blockDim.x + threadIdx.x;
+  for (int i = thread; i < n; i += blockDim.x * blockDim.y) id[i] = ids[i];
   __syncthreads();
   const int32_t own = id[t];
   if (own < 0 || own >= s.V) return;
-  if (threadIdx.x < 64) {  // places of the id's tokens, in order; none if this is not its first
+  if (thread < 64) {  // places of the id's tokens, in order; none if this is not its first
     int m = 0;
     for (int i0 = 0; i0 < n; i0 += 64) {
-      const int i = i0 + threadIdx.x;
+      const int i = i0 + thread;
       const bool is = i < n && id[i] == own;
       const uint64_t all = __ballot(is);
       if (m == 0 && all != 0 && i0 + __ffsll((unsigned long long)all) - 1 != t) break;
-      if (is) same[m + (int)__popcll(all & ((1ull << threadIdx.x) - 1ull))] = i;
+      if (is) same[m + (int)__popcll(all & ((1ull << thread) - 1ull))] = i;
       m += (int)__popcll(all);
     }
-    if (threadIdx.x == 0) found = m;
+    if (thread == 0) found = m;
   }
   __syncthreads();
   const int m = found;
   const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
-  if (m == 0 || c >= s.D) return;
-  const T* d = (const T*)s.dout + c;
+  if (m == 0) return;
+  const T* d = (const T*)s.dout;
+  const int64_t from = min(c, s.D - (WHOLE ? VEC : 1));
   constexpr int AHEAD = 8;
-  float sum[VEC], acc[VEC];
+  float sum[VEC];
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) sum[j] = acc[j] = 0.f;
-  for (int i0 = 0; i0 < m; i0 += AHEAD) {
-    float v[AHEAD][VEC];
+  for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
+  for (int chunk = threadIdx.y * CHUNK; chunk < m; chunk += blockDim.y * CHUNK) {
+    float acc[VEC];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) load<T, VEC>(d + same[min(i0 + u, m - 1)] * s.dout_stride, v[u]);
+    for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
+    const int end = min(chunk + CHUNK, m);
+    for (int i0 = chunk; i0 < end; i0 += AHEAD) {
+      float v[AHEAD][VEC];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (i0 + u < m) {
+      for (int u = 0; u < AHEAD; ++u) load_some<T, VEC, WHOLE>(d + same[min(i0 + u, end - 1)] * s.dout_stride, from, s.D, v[u]);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
-      }
-    if ((i0 + AHEAD) % CHUNK == 0 || i0 + AHEAD >= m) {
+      for (int u = 0; u < AHEAD; ++u)
+        if (i0 + u < end) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) { sum[j] += acc[j]; acc[j] = 0.f; }
+          for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
+        }
     }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] += acc[j];
   }
-  finish<TO, VEC>(s, own, c, sum);
+  if (m > CHUNK) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) others[j * DIRECT_WG + thread] = sum[j];
+    __syncthreads();
+    if (threadIdx.y > 0) return;
+    for (int y = 1; y < (int)blockDim.y && y * CHUNK < m; ++y)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum[j] += others[j * DIRECT_WG + y * blockDim.x + threadIdx.x];
+  }
+  if (threadIdx.y == 0 && c < s.D) finish<TO, VEC, WHOLE, ADD>(s, own, c, sum);
 }
 
-struct Layout { int64_t key[2], pos[2], counts, partial, total; int tiles, passes; };
+struct Layout { int64_t key[2], pos[2], counts, partial, total; int tiles, passes, chunk; };
 Layout layout(int64_t T, int64_t V, int64_t D) {
   Layout L{};
   auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
@@ -403,7 +421,8 @@ Layout layout(int64_t T, int64_t V, int64_t D) {
   while ((V >> (L.passes * BITS)) != 0) ++L.passes;
   for (int i = 0; i < 2; ++i) { L.key[i] = take(T * 4); L.pos[i] = take(T * 4); }
   L.counts = take((int64_t)L.tiles * BINS * 4);
-  L.partial = take(ceil_div(T, CHUNK) * 2 * D * 4);
+  L.chunk = T <= FEW ? FEW_CHUNK : CHUNK;
+  L.partial = take(ceil_div(T, L.chunk) * 2 * D * 4);
   return L;
 }
 
@@ -468,9 +487,16 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
   hipStream_t st = (hipStream_t)hip_stream;
   unsigned char* ws = (unsigned char*)workspace_dev;
   const int64_t eo = type_bytes(table_dtype), ei = type_bytes(dtype);
+  // groups of 8 bfloat16 or 4 float32, by the wider of the two types
+  const int64_t vec = dtype == SIMPLE_BF16 && table_dtype == SIMPLE_BF16 ? 8 : 4;
+  const bool wide = D % vec == 0 && rows_aligned(dout_dev, dout_stride, ei, std::min<int64_t>(16, vec * ei)) &&
+                    rows_aligned(dtable_dev, dtable_stride, eo, std::min<int64_t>(16, vec * eo));
+  const int few_x = std::max(64, std::min(128, shape_of(ceil_div(D, vec))));
+  const dim3 few((unsigned)T, (unsigned)ceil_div(ceil_div(D, vec), few_x));
+  const bool no_sort = T <= DIRECT && T * few.y <= DIRECT_WGS;
   Sort s{ids_dev, nullptr, (int32_t*)(ws + L.key[0]), (int32_t*)(ws + L.pos[0]), (int32_t*)(ws + L.counts), T, V, L.tiles, 0};
   Fill zeros{(unsigned char*)dtable_dev, V, D * eo, dtable_stride * eo, 0};
-  if (T <= DIRECT) {
+  if (no_sort) {
     if (!accumulate) {
       s.n = 0;  // (zeros alone)
       hipLaunchKernelGGL(sort_few_kernel, dim3((unsigned)fill_workgroups(zeros, FEW_WG)), dim3(FEW_WG), 0, st, s, 0, zeros);
@@ -498,31 +524,36 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
     }
   }
   if (T == 0) return launched();
-  Sums m{s.key_in, s.pos_in, dout_dev, dout_stride, T, V, D, scale, dtable_dev, dtable_stride, accumulate, (float*)(ws + L.partial)};
-  // groups of 8 bfloat16 or 4 float32, by the wider of the two types
-  const int64_t vec = dtype == SIMPLE_BF16 && table_dtype == SIMPLE_BF16 ? 8 : 4;
-  const bool wide = D % vec == 0 && rows_aligned(dout_dev, dout_stride, ei, std::min<int64_t>(16, vec * ei)) &&
-                    rows_aligned(dtable_dev, dtable_stride, eo, std::min<int64_t>(16, vec * eo));
-  const int64_t units = wide ? D / vec : D, chunks = ceil_div(T, CHUNK);
+  Sums m{s.key_in, s.pos_in, dout_dev, dout_stride, T, V, D, scale, dtable_dev, dtable_stride, L.chunk, (float*)(ws + L.partial)};
+  const int64_t units = wide ? D / vec : D, chunks = ceil_div(T, L.chunk);
   const int x = std::max(64, shape_of(units));
   const dim3 grid((unsigned)chunks, (unsigned)ceil_div(units, x)), rest((unsigned)(chunks - 1), grid.y);
-  if (grid.y > 65535) return SIMPLE_ECAPACITY;
-  auto go = [&](auto direct, auto sums, auto join) {
-    if (T <= DIRECT) {
-      hipLaunchKernelGGL(direct, dim3((unsigned)T, grid.y), dim3(x), 0, st, m, ids_dev);
+  auto go = [&](auto in, auto out, auto group, auto whole, auto add) {
+    using I = decltype(in);
+    using O = decltype(out);
+    constexpr int N = decltype(group)::value;
+    constexpr bool W = decltype(whole)::value, A = decltype(add)::value;
+    if (no_sort) {
+      hipLaunchKernelGGL((direct_kernel<I, O, N, W, A>), few, dim3(few_x, DIRECT_WG / few_x), 0, st, m, ids_dev);
       return;
     }
-    hipLaunchKernelGGL(sums, grid, dim3(x), 0, st, m);
-    hipLaunchKernelGGL(join, rest, dim3(x), 0, st, m);  // (more than DIRECT tokens are more than one chunk)
+    constexpr int S = W ? N : 1;
+    hipLaunchKernelGGL((sums_kernel<I, O, S, A>), grid, dim3(x), 0, st, m);
+    if (chunks > 1) hipLaunchKernelGGL((join_kernel<O, S, A>), rest, dim3(x), 0, st, m);
   };
-  if (dtype == SIMPLE_BF16 && table_dtype == SIMPLE_BF16) {
-    if (wide) go(direct_kernel<uint16_t, uint16_t, 8>, sums_kernel<uint16_t, uint16_t, 8>, join_kernel<uint16_t, 8>); else go(direct_kernel<uint16_t, uint16_t, 1>, sums_kernel<uint16_t, uint16_t, 1>, join_kernel<uint16_t, 1>);
-  } else if (dtype == SIMPLE_BF16) {
-    if (wide) go(direct_kernel<uint16_t, float, 4>, sums_kernel<uint16_t, float, 4>, join_kernel<float, 4>); else go(direct_kernel<uint16_t, float, 1>, sums_kernel<uint16_t, float, 1>, join_kernel<float, 1>);
-  } else if (table_dtype == SIMPLE_BF16) {
-    if (wide) go(direct_kernel<float, uint16_t, 4>, sums_kernel<float, uint16_t, 4>, join_kernel<uint16_t, 4>); else go(direct_kernel<float, uint16_t, 1>, sums_kernel<float, uint16_t, 1>, join_kernel<uint16_t, 1>);
-  } else {
-    if (wide) go(direct_kernel<float, float, 4>, sums_kernel<float, float, 4>, join_kernel<float, 4>); else go(direct_kernel<float, float, 1>, sums_kernel<float, float, 1>, join_kernel<float, 1>);
-  }
+  auto typed = [&](auto in, auto out, auto group) {
+    auto added = [&](auto whole) {
+      if (accumulate) go(in, out, group, whole, std::true_type{});
+      else go(in, out, group, whole, std::false_type{});
+    };
+    if (wide) added(std::true_type{});
+    else added(std::false_type{});
+  };
+  const std::integral_constant<int, 8> eight;
+  const std::integral_constant<int, 4> four;
+  if (dtype == SIMPLE_BF16 && table_dtype == SIMPLE_BF16) typed((uint16_t)0, (uint16_t)0, eight);
+  else if (dtype == SIMPLE_BF16) typed((uint16_t)0, 0.f, four);
+  else if (table_dtype == SIMPLE_BF16) typed(0.f, (uint16_t)0, four);
+  else typed(0.f, 0.f, four);
   return launched();
 }

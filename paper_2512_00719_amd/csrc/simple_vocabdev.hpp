@@ -41,11 +41,11 @@ template <typename T, int VEC> __device__ __forceinline__ void store(T* p, const
 template <typename T, int VEC, bool WHOLE> __device__ __forceinline__ void load_some(const T* row, int64_t c, int64_t len, float (&out)[VEC]) {
   if constexpr (WHOLE) load<T, VEC>(row + c, out);
   else {
-    static_assert(sizeof(T) * VEC == 16, "16 bytes");
-    typedef unsigned __int128 u128;
-    u128 v = 0;
+    static_assert(sizeof(T) * VEC == 16 || sizeof(T) * VEC == 8, "one access");
+    using Bits = std::conditional_t<sizeof(T) * VEC == 16, unsigned __int128, uint64_t>;
+    Bits v = 0;
     if (len >= VEC) {
-      __builtin_memcpy(&v, row + min(c, len - VEC), 16);
+      __builtin_memcpy(&v, row + min(c, len - VEC), sizeof(v));
       if (c + VEC > len) v >>= 8 * (int)sizeof(T) * (int)(c + VEC - len);
     } else {
 #pragma unroll
@@ -55,12 +55,12 @@ template <typename T, int VEC, bool WHOLE> __device__ __forceinline__ void load_
           x = row[i];
           uint32_t bits = 0;
           __builtin_memcpy(&bits, &x, sizeof(T));
-          v |= (u128)bits << (8 * (int)sizeof(T) * i);
+          v |= (Bits)bits << (8 * (int)sizeof(T) * i);
         }
       }
     }
     T e[VEC];
-    __builtin_memcpy(e, &v, 16);
+    __builtin_memcpy(e, &v, sizeof(v));
 #pragma unroll
     for (int i = 0; i < VEC; ++i) out[i] = up(e[i]);
   }
