@@ -301,7 +301,7 @@ __global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
 }
 
 // The row that chunk blockIdx.x ends inside, if it began there: its partial sums, in order.  12 us where the most frequent of 16,384 tokens has 1300 of them, 41
-// chunks; eight partial rows in flight.
+// chunks; eight partial rows in flight, added in pairs.
 template <typename TO, int VEC, bool ADD>
 __global__ __launch_bounds__(WG) void join_kernel(Sums s) {
   const int64_t chunk = blockIdx.x, e = (chunk + 1) * s.chunk;  // (the grid leaves the last chunk out)
@@ -331,14 +331,13 @@ __global__ __launch_bounds__(WG) void join_kernel(Sums s) {
   for (int64_t k = 0; k < m; k += AHEAD) {
     float v[AHEAD][VEC];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
+    for (int u = 0; u < AHEAD; ++u) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[u][j] = 0.f;
       if (k + u < m) load<float, VEC>(p + 2 * (k + u) * s.D, v[u]);
+    }
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (k + u < m) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
-      }
+    for (int j = 0; j < VEC; ++j) acc[j] += ((v[0][j] + v[1][j]) + (v[2][j] + v[3][j])) + ((v[4][j] + v[5][j]) + (v[6][j] + v[7][j]));
   }
   finish<TO, VEC, true, ADD>(s, id, c, acc);
 }

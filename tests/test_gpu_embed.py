@@ -85,6 +85,28 @@ def test_gradient_strides(pad, shift, dtype):
         assert torch.equal(got, want) and padding_untouched(got, pad, shift)
 
 
+@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("kind", ["uniform", "skewed", "one", "runs", "invalid"])
+@pytest.mark.parametrize("T,V,D", [(512, 700, 1032), (512, 700, 1027), (513, 700, 1032), (511, 90, 3), (409, 600, 5000), (410, 600, 5000), (9, 20, 131_080), (40, 60, 131_080)])
+def test_gradient_with_and_without_a_sort(T, V, D, kind, types):
+    """On both sides of the number of tokens, and of the width, from which on tokens are sorted; the bound as above."""
+    from paper_2512_00719_amd import vocab
+    g = gen(T + D)
+    ids = _ids(T, V, kind, g)
+    dout = normal((T, D), types[0], g)
+    ok = (ids >= 0) & (ids < V)
+    want, size = torch.zeros(V, D, dtype=F64, device=DEV), torch.zeros(V, D, dtype=F64, device=DEV)
+    want.index_add_(0, ids[ok].long(), dout[ok].to(F64))
+    size.index_add_(0, ids[ok].long(), dout[ok].to(F64).abs())
+    arith = (T / 32 + 32 + 3) * 2.0 ** -24
+    got = vocab.embed_grad(ids, dout, V, dtable=torch.full((V, D), 5.0, dtype=types[1], device=DEV))
+    within(got, want, size * arith + want.abs() * HALF[types[1]], "gradient")
+    old = normal((V, D), types[1], g)
+    added = vocab.embed_grad(ids, dout, V, dtable=old.clone(), accumulate=True)
+    total = want + old.to(F64)
+    within(added, total, size * arith + total.abs() * (HALF[types[1]] + 2.0 ** -24), "added gradient")
+
+
 def test_no_tokens():
     from paper_2512_00719_amd import vocab
     table = torch.ones(10, 24, device=DEV)
