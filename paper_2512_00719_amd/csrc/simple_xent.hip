@@ -116,10 +116,14 @@ __global__ __launch_bounds__(S::THREADS) void stats_kernel(Args a) {
                      [&](auto shape, auto& acc, int64_t p0, int64_t q0) { stats_of<decltype(shape)>(a, acc, p0, q0, lds + S::LDS); });
 }
 
-// The tiles' pairs of 16 tokens a workgroup, by FIN_GROUPS groups of tiles, FIN_AHEAD pairs in flight a thread: 5 to 10 us, latency.
-constexpr int FIN_T = 16, FIN_GROUPS = 64, FIN_AHEAD = 8;
-__global__ __launch_bounds__(FIN_T * FIN_GROUPS) void finish_kernel(const Pair* pairs, int nq, int64_t T, int64_t V, const int32_t* targets,
+// The tiles' pairs of FIN_T tokens a workgroup, by groups of tiles, FIN_AHEAD pairs in flight a thread: latency.  Up to FEW_FIN tokens by twos, or one
+// workgroup reads them all (a call of 1 token against 154,187 x 68 18 us, 24 by 16; of 40 against 260,000 x 256 36 and 38; of 128 against 128,256 x 64 20 and 19).
+constexpr int FIN_THREADS = 1024, FIN_AHEAD = 8;
+constexpr int64_t FEW_FIN = 64;
+template <int FIN_T>
+__global__ __launch_bounds__(FIN_THREADS) void finish_kernel(const Pair* pairs, int nq, int64_t T, int64_t V, const int32_t* targets,
                                                                     const float* at_target, float* loss, float* lse) {
+  constexpr int FIN_GROUPS = FIN_THREADS / FIN_T;
   __shared__ Pair part[FIN_GROUPS][FIN_T];
   const int lane = threadIdx.x % FIN_T, grp = threadIdx.x / FIN_T;
   const int64_t t = (int64_t)blockIdx.x * FIN_T + lane;
@@ -880,8 +884,13 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
     for (int64_t v0 = 0; v0 < V; v0 += ALIGN_ROWS)
       stats(aligned_copy<2>(Operand{weight.p + v0 * weight.stride, weight.stride, std::min(ALIGN_ROWS, V - v0)}, D * 2, room + T * a.hidden.stride, st), v0, true);
   }
-  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)ceil_div(T, FIN_T)), dim3(FIN_T * FIN_GROUPS), 0, st, (const Pair*)ws, (int)tiles_q, T, V, targets_dev,
-                     (const float*)a.at_target, loss_dev, lse_dev);
+  auto finish = [&](auto tokens) {
+    constexpr int N = decltype(tokens)::value;
+    hipLaunchKernelGGL((finish_kernel<N>), dim3((unsigned)ceil_div(T, N)), dim3(FIN_THREADS), 0, st, (const Pair*)ws, (int)tiles_q, T, V, targets_dev,
+                       (const float*)a.at_target, loss_dev, lse_dev);
+  };
+  if (T <= FEW_FIN) finish(std::integral_constant<int, 2>{});
+  else finish(std::integral_constant<int, 16>{});
   return launched();
 }
 
