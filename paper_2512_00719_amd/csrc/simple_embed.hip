@@ -244,6 +244,7 @@ struct Sums {
   void* dtable;
   int64_t dtable_stride;
   int chunk;       // sorted places a workgroup of the sums
+  int64_t first;   // the launch's first chunk
   float* partial;  // [chunks][2][D]: of the row that the chunk begins inside, and of the one that it ends inside
 };
 
@@ -261,7 +262,7 @@ template <typename TO, int VEC, bool WHOLE, bool ADD> __device__ __forceinline__
 template <typename T, typename TO, int VEC, bool ADD>
 __global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
   __shared__ int32_t key[CHUNK + 2], pos[CHUNK];
-  const int64_t chunk = blockIdx.x, s0 = chunk * s.chunk;
+  const int64_t chunk = s.first + blockIdx.x, s0 = chunk * s.chunk;
   int m = (int)min((int64_t)s.chunk, s.n - s0);
   for (int i = threadIdx.x; i < s.chunk + 2; i += blockDim.x) {
     const int64_t at = s0 + i - 1;
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
 // chunks; eight partial rows in flight, added in pairs.
 template <typename TO, int VEC, bool ADD>
 __global__ __launch_bounds__(WG) void join_kernel(Sums s) {
-  const int64_t chunk = blockIdx.x, e = (chunk + 1) * s.chunk;  // (the grid leaves the last chunk out)
+  const int64_t chunk = s.first + blockIdx.x, e = (chunk + 1) * s.chunk;  // (the grid leaves the last chunk out)
   const int32_t id = s.key[e - 1];
   if (id >= s.V || s.key[e] != id) return;
   if (s.key[chunk * s.chunk] == id && chunk > 0 && s.key[chunk * s.chunk - 1] == id) return;
@@ -455,11 +456,15 @@ extern "C" int simple_embed(const int32_t* ids_dev, const void* table_dev, int64
   // (rows that are not aligned: bfloat16 by unaligned loads, 19 us for 8192 rows of 2047 values against 26 by single elements)
   const int64_t units = wide || dtype == SIMPLE_BF16 ? ceil_div(D, 16 / e) : D;
   const int x = shape_of(units), y = WG / x;
-  const dim3 grid((unsigned)ceil_div(T, (int64_t)y * RD), (unsigned)ceil_div(units, x)), block(x, y);
-  if (grid.y > 65535) return SIMPLE_ECAPACITY;
+  if (ceil_div(units, x) > 65535) return SIMPLE_ECAPACITY;
   auto go = [&](auto kernel, auto* type) {
     using T_ = std::remove_pointer_t<decltype(type)>;
-    hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)hip_stream, ids_dev, (const T_*)table_dev, table_stride, T, V, D, scale, (T_*)out_dev, out_stride);
+    const int64_t most = LAUNCH_WGS * y * RD;
+    for (int64_t t0 = 0; t0 < T; t0 += most) {
+      const int64_t n = std::min(most, T - t0);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(n, (int64_t)y * RD), (unsigned)ceil_div(units, x)), dim3(x, y), 0, (hipStream_t)hip_stream, ids_dev + t0,
+                         (const T_*)table_dev, table_stride, n, V, D, scale, (T_*)out_dev + t0 * out_stride, out_stride);
+    }
   };
   if (dtype == SIMPLE_F32) { if (wide) go(lookup_kernel<float, 4, true>, (float*)0); else go(lookup_kernel<float, 1, true>, (float*)0); }
   else { if (wide) go(lookup_kernel<uint16_t, 8, true>, (uint16_t*)0); else go(lookup_kernel<uint16_t, 8, false>, (uint16_t*)0); }
@@ -495,18 +500,23 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
   const bool no_sort = T <= DIRECT && T * few.y <= DIRECT_WGS;
   Sort s{ids_dev, nullptr, (int32_t*)(ws + L.key[0]), (int32_t*)(ws + L.pos[0]), (int32_t*)(ws + L.counts), T, V, L.tiles, 0};
   Fill zeros{(unsigned char*)dtable_dev, V, D * eo, dtable_stride * eo, 0};
+  auto zeros_alone = [&](int64_t shares, int threads) {  // from share zeros.first on
+    Sort none = s;
+    none.n = 0;
+    for (; shares > 0; shares -= LAUNCH_WGS, zeros.first += LAUNCH_WGS)
+      hipLaunchKernelGGL(sort_few_kernel, dim3((unsigned)std::min(shares, LAUNCH_WGS)), dim3(threads), 0, st, none, 0, zeros);
+  };
   if (no_sort) {
-    if (!accumulate) {
-      s.n = 0;  // (zeros alone)
-      hipLaunchKernelGGL(sort_few_kernel, dim3((unsigned)fill_workgroups(zeros, FEW_WG)), dim3(FEW_WG), 0, st, s, 0, zeros);
-    }
+    if (!accumulate) zeros_alone(fill_workgroups(zeros, FEW_WG), FEW_WG);
   } else if (T <= FEW) {
-    const int64_t shares = accumulate ? 0 : fill_workgroups(zeros, FEW_WG);
+    const int64_t all = accumulate ? 0 : fill_workgroups(zeros, FEW_WG), shares = std::min(all, LAUNCH_WGS);
     hipLaunchKernelGGL(sort_few_kernel, dim3((unsigned)(shares + 1)), dim3(FEW_WG), 0, st, s, L.passes, zeros);
+    zeros.first = shares;
+    zeros_alone(all - shares, FEW_WG);
     s.key_in = s.key_out; s.pos_in = s.pos_out;
   } else {
     const int kernels = 2 * L.passes;
-    const int64_t shares = accumulate ? 0 : fill_workgroups(zeros, WG);
+    const int64_t all = accumulate ? 0 : fill_workgroups(zeros, WG), shares = std::min(all, kernels * LAUNCH_WGS);
     int kernel = 0;
     auto beside = [&](auto* f) {  // the kernel's share of the zeros, behind its own workgroups
       zeros.first = shares * kernel / kernels;
@@ -521,12 +531,14 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
       s.key_out = (int32_t*)(ws + L.key[(p + 1) & 1]); s.pos_out = (int32_t*)(ws + L.pos[(p + 1) & 1]);
       s.shift += BITS;
     }
+    zeros.first = shares;
+    zeros_alone(all - shares, WG);
   }
   if (T == 0) return launched();
-  Sums m{s.key_in, s.pos_in, dout_dev, dout_stride, T, V, D, scale, dtable_dev, dtable_stride, L.chunk, (float*)(ws + L.partial)};
+  Sums m{s.key_in, s.pos_in, dout_dev, dout_stride, T, V, D, scale, dtable_dev, dtable_stride, L.chunk, 0, (float*)(ws + L.partial)};
   const int64_t units = wide ? D / vec : D, chunks = ceil_div(T, L.chunk);
   const int x = std::max(64, shape_of(units));
-  const dim3 grid((unsigned)chunks, (unsigned)ceil_div(units, x)), rest((unsigned)(chunks - 1), grid.y);
+  const unsigned across = (unsigned)ceil_div(units, x);
   auto go = [&](auto in, auto out, auto group, auto whole, auto add) {
     using I = decltype(in);
     using O = decltype(out);
@@ -537,8 +549,10 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
       return;
     }
     constexpr int S = W ? N : 1;
-    hipLaunchKernelGGL((sums_kernel<I, O, S, A>), grid, dim3(x), 0, st, m);
-    if (chunks > 1) hipLaunchKernelGGL((join_kernel<O, S, A>), rest, dim3(x), 0, st, m);
+    for (m.first = 0; m.first < chunks; m.first += LAUNCH_WGS)
+      hipLaunchKernelGGL((sums_kernel<I, O, S, A>), dim3((unsigned)std::min(LAUNCH_WGS, chunks - m.first), across), dim3(x), 0, st, m);
+    for (m.first = 0; m.first < chunks - 1; m.first += LAUNCH_WGS)
+      hipLaunchKernelGGL((join_kernel<O, S, A>), dim3((unsigned)std::min(LAUNCH_WGS, chunks - 1 - m.first), across), dim3(x), 0, st, m);
   };
   auto typed = [&](auto in, auto out, auto group) {
     auto added = [&](auto whole) {

@@ -292,7 +292,7 @@ template <typename F> void typed(int dtype, bool whole, F&& f) {
 
 bool bad_rows(const void* p, int64_t stride, int64_t D) { return p == nullptr || stride < D; }
 
-template <int OUT> int launch_rows(const Args& a, int dtype, hipStream_t st) {
+template <int OUT> int launch_rows(Args a, int dtype, hipStream_t st) {
   const int64_t e = type_bytes(dtype);
   const int64_t vec = 16 / e;
   const bool whole = a.D % vec == 0 && rows_aligned(a.x, a.x_stride, e, 16) && rows_aligned(a.residual, a.residual_stride, e, 16) &&
@@ -303,7 +303,18 @@ template <int OUT> int launch_rows(const Args& a, int dtype, hipStream_t st) {
       using T = std::remove_pointer_t<decltype(type)>;
       constexpr int NT = decltype(nt)::value, VEC = decltype(vec)::value, NV = decltype(ept)::value / VEC;
       constexpr int ROWS = NT > WG ? 1 : WG / NT;
-      hipLaunchKernelGGL((rows_kernel<T, VEC, decltype(aligned)::value, NT, NV, OUT>), dim3((unsigned)ceil_div(a.T, ROWS)), dim3(NT > WG ? NT : WG), 0, st, a);
+      constexpr int64_t E = sizeof(T), OE = OUT == NORM ? E : 1;
+      auto on = [](auto* p, int64_t bytes) { return p ? (decltype(p))((uintptr_t)p + (uintptr_t)bytes) : p; };
+      for (int64_t left = a.T; left > 0; left -= a.T) {
+        a.T = left < ROWS * LAUNCH_WGS ? left : ROWS * LAUNCH_WGS;
+        hipLaunchKernelGGL((rows_kernel<T, VEC, decltype(aligned)::value, NT, NV, OUT>), dim3((unsigned)ceil_div(a.T, ROWS)), dim3(NT > WG ? NT : WG), 0, st, a);
+        a.x = on(a.x, a.T * a.x_stride * E);
+        a.residual = on(a.residual, a.T * a.residual_stride * E);
+        a.h = on(a.h, a.T * a.h_stride * E);
+        a.out = on(a.out, a.T * a.out_stride * OE);
+        a.rstd = on(a.rstd, a.T * (int64_t)sizeof(float));
+        a.scales = on(a.scales, a.T * (int64_t)sizeof(float));
+      }
     });
   });
   return launched();

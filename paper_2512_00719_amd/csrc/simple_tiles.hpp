@@ -424,6 +424,7 @@ inline int tiles_for(int64_t p, int64_t q) {
   const double rounds = (double)(large / CUS) + (last == 0 ? 0.0 : last * 4 <= CUS ? 0.35 : 1.0);
   return rounds <= 0.625 * (double)ceil_div(small, 2 * CUS) ? TILE_256 : TILE_128;
 }
+inline int64_t tile_rows(int tiles) { return (int64_t)16 << (tiles - TILE_16); }
 inline int64_t tile_columns(int tiles) { return tiles <= TILE_32 ? 64 : tiles <= TILE_128 ? 128 : 256; }
 template <class E, typename F> void shaped(int tiles, F&& f) {
   if (tiles == TILE_16) f(Shape<E, 16, 64, 1, 4, 4>{});

@@ -122,6 +122,8 @@ inline bool rows_aligned(const void* p, int64_t stride, int64_t esz, int64_t to)
   return p == nullptr || (((uintptr_t)p & (uintptr_t)(to - 1)) == 0 && ((stride * esz) & (to - 1)) == 0);
 }
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Workgroups of a launch at most, of up to 1024 threads: of a grid of 2^32 threads or more the runtime starts what is left modulo 2^32, without an error.
+constexpr int64_t LAUNCH_WGS = (int64_t)1 << 21;
 inline int launched() { return hipGetLastError() == hipSuccess ? SIMPLE_OK : SIMPLE_EDEVICE; }
 
 }  // namespace vocab

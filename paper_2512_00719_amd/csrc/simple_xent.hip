@@ -873,10 +873,14 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
       else hipLaunchKernelGGL((stats_kernel<S, false>), grid, block, 0, st, a);
     });
   };
+  auto pieces = [&](bool dir) {  // one, but for tens of thousands of tokens against millions of weights
+    const int64_t most = LAUNCH_WGS / ceil_div(T, tile_rows(tiles)) * columns;
+    for (int64_t v0 = 0; v0 < V; v0 += most) stats(Operand{weight.p + v0 * weight.stride, weight.stride, std::min(most, V - v0)}, v0, dir);
+  };
   if (direct(a.hidden, a.k_bytes) && direct(weight, a.k_bytes)) {
-    stats(weight, 0, true);
+    pieces(true);
   } else if (T <= FEW_TOKENS) {
-    stats(weight, 0, false);
+    pieces(false);
   } else {  // copies with aligned rows, of the weights ALIGN_ROWS (a multiple of every tile) at a time
     unsigned char* room = ws + pairs_bytes(T, V) + ((T * 4 + 255) & ~(int64_t)255);
     a.hidden = aligned_copy<2>(a.hidden, D * 2, room, st);
