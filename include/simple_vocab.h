@@ -69,8 +69,8 @@ int simple_embed(const int32_t* ids_dev, const void* table_dev, int64_t table_st
 
 /*
  * Its gradient: dtable[v, :] = scale * (sum of dout[t, :] over the tokens t with ids[t] = v), written whole (rows without a token
- * become zeros), or with accumulate != 0 added to what dtable holds (rows without a token are not touched).  The tokens are
- * sorted by id, and a row's sum is formed in float32 in an order that depends on ids and T alone.  Ids outside [0, V) are
+ * become zeros), or with accumulate != 0 added to what dtable holds (rows without a token are not touched).  A row's sum is formed
+ * in float32 in an order that depends on ids and T alone (a table formed by blocks of columns has the bits of the whole one).  Ids outside [0, V) are
  * ignored.  dout has type dtype, dtable table_dtype.  workspace_dev: simple_embed_grad_workspace(T, V, D) bytes, 16-byte aligned.
  * T < 2^31, V < 2^31 - 1.
  */

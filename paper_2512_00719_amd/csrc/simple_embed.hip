@@ -2,9 +2,10 @@
 //
 // Lookup: bound by memory, one read and one write of a row's bytes; nothing is computed but the scale.
 //
-// Gradient: the tokens are sorted by id (stable, so that a row's tokens keep their order), then summed in chunks of CHUNK sorted
-// places.  A row whose tokens lie within a chunk is finished there; one that runs on leaves a partial sum in each chunk, and the
-// chunk that it began in joins them in order.  No atomics on sums: results do not depend on the order of workgroups.  A
+// Gradient: the tokens are sorted by id (stable, so that a row's tokens keep their order; few tokens are found where a sort would put them), then summed in chunks of CHUNK sorted
+// places (FEW_CHUNK up to FEW tokens).  A row whose tokens lie within a chunk is finished there; one that runs on leaves a partial sum in each chunk, and the
+// chunk that it began in joins them in order.  No atomics on sums: a row's order of additions depends on the ids and their number alone, not
+// on the order of workgroups, on the width or on the types.  A
 // frequent token (8 % of a text's tokens are one word) is so spread over many workgroups.
 // Bound: the zeros of the rows without a token, V * D values, are most of what is written.
 #include <algorithm>
@@ -301,6 +302,10 @@ __global__ __launch_bounds__(WG) void sums_kernel(Sums s) {
   }
 }
 
+// Chunks' sums of a row behind its first chunk's are added JOIN at a time, in pairs; zeros where there are no more.
+constexpr int JOIN = 8;
+__device__ __forceinline__ float joined(const float (&v)[JOIN]) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
+
 // The row that chunk blockIdx.x ends inside, if it began there: its partial sums, in order.  12 us where the most frequent of 16,384 tokens has 1300 of them, 41
 // chunks; eight partial rows in flight, added in pairs.
 template <typename TO, int VEC, bool ADD>
@@ -328,32 +333,39 @@ __global__ __launch_bounds__(WG) void join_kernel(Sums s) {
   load<float, VEC>(s.partial + (2 * chunk + 1) * s.D + c, acc);
   const float* p = s.partial + 2 * (chunk + 1) * s.D + c;
   const int64_t m = end - chunk;
-  constexpr int AHEAD = 8;
-  for (int64_t k = 0; k < m; k += AHEAD) {
-    float v[AHEAD][VEC];
+  for (int64_t k = 0; k < m; k += JOIN) {
+    float v[JOIN][VEC];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
+    for (int u = 0; u < JOIN; ++u) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) v[u][j] = 0.f;
       if (k + u < m) load<float, VEC>(p + 2 * (k + u) * s.D, v[u]);
     }
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) acc[j] += ((v[0][j] + v[1][j]) + (v[2][j] + v[3][j])) + ((v[4][j] + v[5][j]) + (v[6][j] + v[7][j]));
+    for (int j = 0; j < VEC; ++j) {
+      float w[JOIN];
+#pragma unroll
+      for (int u = 0; u < JOIN; ++u) w[u] = v[u][j];
+      acc[j] += joined(w);
+    }
   }
   finish<TO, VEC, true, ADD>(s, id, c, acc);
 }
 
-// Up to DIRECT tokens need no sort: the workgroup of an id's first token finds the others and sums them in their order, CHUNK at a time, chunks in turn by the groups of
-// `blockDim.x` threads, whose sums are joined in the groups' order.  One kernel where five steps of 3 to 5 us each would wait for each other (a call with 219 tokens of
+// Up to DIRECT tokens need no sort: the workgroup of an id's first token finds the others, and from how many tokens have lower ids where a sort would put them, and sums
+// them in the same chunks and joins those in the same order as the two kernels above, so that no bit depends on which way is taken.  Chunks go to the groups of
+// `blockDim.x` threads in turn (512 tokens of one id, 1024 values: 24.2 us of kernels, 20.7 with chunks counted from the row's first token and joined by groups, in an order that
+// changed with the width; of 512 ids 6.7 and 6.6).  One kernel where five steps of 3 to 5 us each would wait for each other (a call with 219 tokens of
 // 89 values float32 26 us sorted, 14 so; 300 and 512 of 1024 bfloat16 33 and 15).  Every token has its workgroups: no more than DIRECT_WGS, two rounds of the chip
 // (512 tokens of 7172 values, 4096 workgroups: 28 us sorted, 36 so).  600 tokens of 1024 values took 18 us this way, but 46 with one id in most of them, 28 sorted.
-constexpr int DIRECT = 512, DIRECT_WG = 512;
+constexpr int DIRECT = 512, DIRECT_WG = 512, DIRECT_X = 128;  // DIRECT_X: threads along a row at most
+static_assert(DIRECT <= FEW, "chunks of FEW_CHUNK");
 constexpr int64_t DIRECT_WGS = 2048;
 template <typename T, typename TO, int VEC, bool WHOLE, bool ADD>
 __global__ __launch_bounds__(DIRECT_WG) void direct_kernel(Sums s, const int32_t* ids) {
   __shared__ int32_t id[DIRECT], same[DIRECT];
-  __shared__ int found;
-  __shared__ float others[DIRECT_WG * VEC];
+  __shared__ int found, ahead;
+  __shared__ float others[JOIN * VEC * DIRECT_X];
   const int t = blockIdx.x, n = (int)s.n, thread = threadIdx.y * blockDim.x + threadIdx.x;
   for (int i = thread; i < n; i += blockDim.x * blockDim.y) id[i] = ids[i];
   __syncthreads();
@@ -370,6 +382,12 @@ __global__ __launch_bounds__(DIRECT_WG) void direct_kernel(Sums s, const int32_t
       m += (int)__popcll(all);
     }
     if (thread == 0) found = m;
+  } else if (thread < 128) {  // how many tokens a sort would have ahead of them
+    int low = 0;
+    for (int i = thread - 64; i < n; i += 64) low += (uint32_t)id[i] < (uint32_t)own;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) low += __shfl_xor(low, o, 64);
+    if (thread == 64) ahead = low;
   }
   __syncthreads();
   const int m = found;
@@ -377,16 +395,11 @@ __global__ __launch_bounds__(DIRECT_WG) void direct_kernel(Sums s, const int32_t
   if (m == 0) return;
   const T* d = (const T*)s.dout;
   const int64_t from = min(c, s.D - (WHOLE ? VEC : 1));
-  constexpr int AHEAD = 8;
-  float sum[VEC];
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
-  for (int chunk = threadIdx.y * CHUNK; chunk < m; chunk += blockDim.y * CHUNK) {
-    float acc[VEC];
+  auto sum = [&](int begin, int end, float (&acc)[VEC]) {
+    constexpr int AHEAD = 8;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
-    const int end = min(chunk + CHUNK, m);
-    for (int i0 = chunk; i0 < end; i0 += AHEAD) {
+    for (int i0 = begin; i0 < end; i0 += AHEAD) {
       float v[AHEAD][VEC];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) load_some<T, VEC, WHOLE>(d + same[min(i0 + u, end - 1)] * s.dout_stride, from, s.D, v[u]);
@@ -397,19 +410,32 @@ __global__ __launch_bounds__(DIRECT_WG) void direct_kernel(Sums s, const int32_t
           for (int j = 0; j < VEC; ++j) acc[j] += v[u][j];
         }
     }
+  };
+  // The row's first chunk ends where a sort's would.  JOIN of those behind it at a time, by groups in turn, the first group last.
+  const int first = min(m, s.chunk - (ahead & (s.chunk - 1))), groups = blockDim.y, group = (threadIdx.y - 1) & (groups - 1);
+  float acc[VEC];
+  if (threadIdx.y == 0) sum(0, first, acc);
+  for (int k0 = first; k0 < m; k0 += JOIN * s.chunk) {
+    for (int u = group; u < JOIN; u += groups) {
+      float v[VEC];
+      const int begin = k0 + u * s.chunk;
+      sum(begin, min(begin + s.chunk, m), v);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) sum[j] += acc[j];
-  }
-  if (m > CHUNK) {
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) others[j * DIRECT_WG + thread] = sum[j];
+      for (int j = 0; j < VEC; ++j) others[(u * VEC + j) * DIRECT_X + threadIdx.x] = v[j];
+    }
     __syncthreads();
-    if (threadIdx.y > 0) return;
-    for (int y = 1; y < (int)blockDim.y && y * CHUNK < m; ++y)
+    if (threadIdx.y == 0) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[j] += others[j * DIRECT_WG + y * blockDim.x + threadIdx.x];
+      for (int j = 0; j < VEC; ++j) {
+        float v[JOIN];
+#pragma unroll
+        for (int u = 0; u < JOIN; ++u) v[u] = others[(u * VEC + j) * DIRECT_X + threadIdx.x];
+        acc[j] += joined(v);
+      }
+    }
+    __syncthreads();
   }
-  if (threadIdx.y == 0 && c < s.D) finish<TO, VEC, WHOLE, ADD>(s, own, c, sum);
+  if (threadIdx.y == 0 && c < s.D) finish<TO, VEC, WHOLE, ADD>(s, own, c, acc);
 }
 
 struct Layout { int64_t key[2], pos[2], counts, partial, total; int tiles, passes, chunk; };
@@ -495,7 +521,7 @@ extern "C" int simple_embed_grad(const int32_t* ids_dev, const void* dout_dev, i
   const int64_t vec = dtype == SIMPLE_BF16 && table_dtype == SIMPLE_BF16 ? 8 : 4;
   const bool wide = D % vec == 0 && rows_aligned(dout_dev, dout_stride, ei, std::min<int64_t>(16, vec * ei)) &&
                     rows_aligned(dtable_dev, dtable_stride, eo, std::min<int64_t>(16, vec * eo));
-  const int few_x = std::max(64, std::min(128, shape_of(ceil_div(D, vec))));
+  const int few_x = std::max(64, std::min(DIRECT_X, shape_of(ceil_div(D, vec))));
   const dim3 few((unsigned)T, (unsigned)ceil_div(ceil_div(D, vec), few_x));
   const bool no_sort = T <= DIRECT && T * few.y <= DIRECT_WGS;
   Sort s{ids_dev, nullptr, (int32_t*)(ws + L.key[0]), (int32_t*)(ws + L.pos[0]), (int32_t*)(ws + L.counts), T, V, L.tiles, 0};
