@@ -5,6 +5,9 @@ A decoding step is ``embed`` -> the model -> ``rms_norm_int8`` -> ``linear_int8`
 ``linear_xent_grad`` -> ``rms_norm_grad`` ... ``embed_grad``.  As in ``binding`` only arguments are checked and marshalled here:
 every step runs in the HIP kernels of the library, on the current stream, without a synchronisation.  Outputs and workspaces are allocated by torch
 where they are not passed.
+
+Automatic differentiation records none of these calls: gradients are calls of their own.  A tensor that requires a gradient is refused (``ValueError``) unless gradients
+are off (``torch.no_grad()``), so that a loss does not silently lose a term; a tensor that is passed for an output counts as modified in place.
 """
 from __future__ import annotations
 
@@ -62,9 +65,16 @@ def _dtype(t: torch.Tensor, name: str) -> int:
         raise TypeError(f"{name} is float32 or bfloat16, got {t.dtype}") from None
 
 
+def _refuse_recording(name: str) -> None:
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which this call does not record: pass it detached, or call under torch.no_grad()")
+
+
 # (These run ahead of every call, whose kernels may take 5 us: the usual case is one expression.)
 def _tensor(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
     """`t`, if it is a tensor of that kind on that device whose rows are dense (the last dimension's stride is 1)."""
+    if t.requires_grad:
+        _refuse_recording(name)
     if t.dtype is dtype and t.shape == shape and t.device == device and (t.is_contiguous() or t.stride(-1) == 1 or t.shape[-1] == 1):
         return t
     if t.dtype is not dtype:
@@ -82,6 +92,8 @@ def _matrix(t: torch.Tensor, name: str, dtypes=(torch.float32, torch.bfloat16)) 
         raise ValueError(f"{name} is [rows, values], got shape {tuple(t.shape)}")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} is one of {dtypes}, got {t.dtype}")
+    if t.requires_grad:
+        _refuse_recording(name)
     device = t.device
     if device.type != "cuda" or device.index != torch._C._cuda_getDevice():
         raise ValueError(f"{name} is on {device}: the current GPU is wanted")
@@ -102,11 +114,12 @@ def _ptr(t: Optional[torch.Tensor]) -> int:
 
 
 def _out(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
-    return torch.empty(shape, dtype=dtype, device=device) if t is None else _tensor(t, name, shape, dtype, device)
-
-
-def _like(t: Optional[torch.Tensor], name: str, other: torch.Tensor) -> torch.Tensor:
-    return torch.empty(other.shape, dtype=other.dtype, device=other.device) if t is None else _tensor(t, name, other.shape, other.dtype, other.device)
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _tensor(t, name, shape, dtype, device)
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+    return t
 
 
 def _workspace(nbytes: int, where: str, device: torch.device) -> torch.Tensor:
@@ -205,7 +218,7 @@ def embed_grad(ids, dout, V: int, *, scale: float = 1.0, dtable=None, accumulate
         dtable = torch.empty((V, D), dtype=dout.dtype, device=dout.device)
     else:
         _dtype(dtable, "dtable")
-        _tensor(dtable, "dtable", (V, D), dtable.dtype, dout.device)
+        _out(dtable, "dtable", (V, D), dtable.dtype, dout.device)
     ws = _workspace(_lib.simple_embed_grad_workspace(T, V, D), "simple_embed_grad_workspace", dout.device)
     _check(_lib.simple_embed_grad(ids.data_ptr(), dout.data_ptr(), _stride(dout), T, V, D, _TYPES[dout.dtype], scale, dtable.data_ptr(),
                                   _stride(dtable), _TYPES[dtable.dtype], int(accumulate), ws.data_ptr(), ws.numel(), _current_stream()),
@@ -272,7 +285,7 @@ def linear_xent_grad(dloss, hidden, weight, targets, lse, *, logit_scale: float 
         dweight = torch.empty((V, D), dtype=torch.bfloat16, device=hidden.device)
     else:
         _dtype(dweight, "dweight")
-        _tensor(dweight, "dweight", (V, D), dweight.dtype, hidden.device)
+        _out(dweight, "dweight", (V, D), dweight.dtype, hidden.device)
     ws = _workspace(_lib.simple_xent_grad_workspace(T, V, D, int(need_dhidden), int(need_dweight)), "simple_xent_grad_workspace", hidden.device)
     _check(_lib.simple_xent_grad(dloss.data_ptr(), hidden.data_ptr(), _stride(hidden), weight.data_ptr(), _stride(weight), targets.data_ptr(),
                                  lse.data_ptr(), T, V, D, logit_scale, _ptr(dhidden), _stride(dhidden), _ptr(dweight), _stride(dweight),
