@@ -96,26 +96,30 @@ int64_t simple_linear_int8_workspace(int64_t T, int64_t V, int64_t K);
  * matrix is kept:
  *   lse[t] = log(sum over v of exp z[t, v]),   loss[t] = lse[t] - z[t, targets[t]]
  * loss is the negative log-probability of the target, 0 where the target is outside [0, V) (a token that is masked).  logit_scale (positive) is
- * 1 / temperature for tokens that were drawn at one.  workspace_dev: simple_xent_workspace(T, V, D) bytes, 16-byte aligned.  T <= 2^20, V <= 2^28, D <= 65536, and
+ * 1 / temperature for tokens that were drawn at one.  workspace_dev: simple_xent_workspace(T, V, D) bytes, 16-byte aligned; where the rows of hidden and weight are
+ * 16-byte aligned (D and the strides multiples of 8, strides of 2^21 at most) nothing is copied and simple_xent_workspace_aligned(T, V, D) do.  T <= 2^20, V <= 2^28, D <= 65536, and
  * T * V < 2^41.
  */
 int simple_xent(const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, const int32_t* targets_dev,
                 int64_t T, int64_t V, int64_t D, float logit_scale, float* loss_dev, float* lse_dev, void* workspace_dev,
                 int64_t workspace_bytes, void* hip_stream);
 int64_t simple_xent_workspace(int64_t T, int64_t V, int64_t D);
+int64_t simple_xent_workspace_aligned(int64_t T, int64_t V, int64_t D);
 
 /*
  * Its gradient for a loss of sum over t of dloss[t] * loss[t]: with G[t, v] = logit_scale * dloss[t] * (exp(z[t, v] - lse[t]) - [v = targets[t]]),
  *   dhidden = G * weight (bfloat16),   dweight = transposed G * hidden (dweight_dtype; accumulate != 0 adds it to what is there)
  * lse_dev is what simple_xent wrote.  Logits are formed again, a piece of the vocabulary at a time, and G is rounded to 11 bits or more for the products.
  * A token whose target is outside [0, V) or whose dloss is 0 takes no part whatever its states hold: its row of dhidden is zeros.
- * Either output may be NULL: then it is not formed.  workspace_dev: simple_xent_grad_workspace() bytes for the outputs wanted, 16-byte aligned.
+ * Either output may be NULL: then it is not formed.  workspace_dev: simple_xent_grad_workspace() bytes for the outputs wanted, 16-byte aligned
+ * (simple_xent_grad_workspace_aligned() where the rows of hidden and weight are, as above).
  */
 int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride,
                      const int32_t* targets_dev, const float* lse_dev, int64_t T, int64_t V, int64_t D, float logit_scale, void* dhidden_dev,
                      int64_t dhidden_stride, void* dweight_dev, int64_t dweight_stride, int dweight_dtype, int accumulate,
                      void* workspace_dev, int64_t workspace_bytes, void* hip_stream);
 int64_t simple_xent_grad_workspace(int64_t T, int64_t V, int64_t D, int want_dhidden, int want_dweight);
+int64_t simple_xent_grad_workspace_aligned(int64_t T, int64_t V, int64_t D, int want_dhidden, int want_dweight);
 
 #ifdef __cplusplus
 }

@@ -739,12 +739,14 @@ int hidden_splits(int64_t T, int64_t V, int64_t D) {
 
 constexpr int64_t WEIGHT_WGS = 2048;  // workgroups that look for the weights' largest magnitude
 struct Layout { int64_t copy_h, copy_w, tops, partial, tokens, g, gt, wt, ht, sums, total, rows, t16; int splits; };
-Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
+// Totals are in whole pieces of 64 KB: a small call's is the same whether rows are aligned or not.
+int64_t in_pieces(int64_t bytes) { return ceil_div(bytes, 65536) * 65536; }
+Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight, bool copies) {
   Layout L{};
   auto take = [&](int64_t bytes) { const int64_t at = L.total; L.total += (bytes + 255) & ~(int64_t)255; return at; };
   L.rows = piece_rows(T, V);
   L.t16 = ceil_div(T, 16) * 16;
-  if (T > FEW_TOKENS) {  // (for rows that are not aligned)
+  if (copies) {
     L.copy_h = take(T * aligned_stride(D * 2));
     L.copy_w = take(L.rows * aligned_stride(D * 2));
   }
@@ -761,6 +763,7 @@ Layout layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight) {
     L.gt = take(L.rows * L.t16 * 2);
     L.ht = take(D * L.t16 * 2);
   }
+  L.total = in_pieces(L.total);
   return L;
 }
 
@@ -787,6 +790,7 @@ FewLayout few_layout(int64_t T, int64_t V, int64_t D, bool hidden, bool weight, 
     L.gt = take(2 * L.rows * L.t_pad * 2);
     L.ht = take(D * L.t_pad * 2);
   }
+  L.total = in_pieces(L.total);
   return L;
 }
 
@@ -830,13 +834,25 @@ bool good_scale(float s) { return s > 0.f && s <= 3.4e38f; }
 // (Tiles are numbered in 32 bits.)
 bool too_many_tiles(int64_t T, int64_t V) { return ceil_div(T, 16) * ceil_div(V, 64) > (int64_t)0x7FFFFFFF; }
 int64_t pairs_bytes(int64_t T, int64_t V) { return ((ceil_div(V, tile_columns(tiles_for(T, V))) * T * (int64_t)sizeof(Pair) + 255) & ~(int64_t)255); }
+// What a call needs beyond the sizes' least: copies of operands whose rows are not aligned (`fits`: both are).
+int64_t xent_bytes(int64_t T, int64_t V, int64_t D, bool fits) {
+  const int64_t copies = !fits && T > FEW_TOKENS ? (T + std::min(V, ALIGN_ROWS)) * aligned_stride(D * 2) : 0;
+  return in_pieces(pairs_bytes(T, V) + ((T * 4 + 255) & ~(int64_t)255) + copies);
+}
+int64_t grad_bytes(int64_t T, int64_t V, int64_t D, bool hidden, bool weight, bool fits) {
+  if (T > FEW_GRAD || T == 0) return layout(T, V, D, hidden, weight, !fits && T > FEW_TOKENS).total;
+  const int64_t least = few_layout(T, V, D, hidden, weight, false).total;
+  return fits ? least : std::max(least, few_layout(T, V, D, hidden, weight, true).total);
+}
 }  // namespace
 
 extern "C" int64_t simple_xent_workspace(int64_t T, int64_t V, int64_t D) {
   const int rc = check_sizes(T, V, D);
-  if (rc != SIMPLE_OK) return rc;
-  const int64_t copies = T > FEW_TOKENS ? (T + std::min(V, ALIGN_ROWS)) * aligned_stride(D * 2) : 0;
-  return pairs_bytes(T, V) + ((T * 4 + 255) & ~(int64_t)255) + copies;
+  return rc != SIMPLE_OK ? rc : xent_bytes(T, V, D, false);
+}
+extern "C" int64_t simple_xent_workspace_aligned(int64_t T, int64_t V, int64_t D) {
+  const int rc = check_sizes(T, V, D);
+  return rc != SIMPLE_OK ? rc : xent_bytes(T, V, D, true);
 }
 
 extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride, const int32_t* targets_dev,
@@ -848,12 +864,13 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
   if (T == 0) return SIMPLE_OK;
   if (!hidden_dev || !weight_dev || !targets_dev || !loss_dev || !lse_dev) return SIMPLE_EINVAL;
   if (!workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
-  if (too_many_tiles(T, V) || workspace_bytes < simple_xent_workspace(T, V, D)) return SIMPLE_ECAPACITY;
-  hipStream_t st = (hipStream_t)hip_stream;
-  unsigned char* ws = (unsigned char*)workspace_dev;
   Args a{};
   a.hidden = {(const unsigned char*)hidden_dev, hidden_stride * 2, T};
   const Operand weight{(const unsigned char*)weight_dev, weight_stride * 2, V};
+  const bool fits = direct(a.hidden, D * 2) && direct(weight, D * 2);
+  if (too_many_tiles(T, V) || workspace_bytes < xent_bytes(T, V, D, fits)) return SIMPLE_ECAPACITY;
+  hipStream_t st = (hipStream_t)hip_stream;
+  unsigned char* ws = (unsigned char*)workspace_dev;
   a.k_bytes = (int)(D * 2);
   a.scale = logit_scale;
   a.targets = targets_dev;
@@ -877,7 +894,7 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
     const int64_t most = LAUNCH_WGS / ceil_div(T, tile_rows(tiles)) * columns;
     for (int64_t v0 = 0; v0 < V; v0 += most) stats(Operand{weight.p + v0 * weight.stride, weight.stride, std::min(most, V - v0)}, v0, dir);
   };
-  if (direct(a.hidden, a.k_bytes) && direct(weight, a.k_bytes)) {
+  if (fits) {
     pieces(true);
   } else if (T <= FEW_TOKENS) {
     pieces(false);
@@ -901,8 +918,12 @@ extern "C" int simple_xent(const void* hidden_dev, int64_t hidden_stride, const 
 extern "C" int64_t simple_xent_grad_workspace(int64_t T, int64_t V, int64_t D, int want_dhidden, int want_dweight) {
   const int rc = check_sizes(T, V, D);
   if (rc != SIMPLE_OK) return rc;
-  const bool h = want_dhidden != 0, w = want_dweight != 0;
-  return T > FEW_GRAD || T == 0 ? layout(T, V, D, h, w).total : std::max(few_layout(T, V, D, h, w, false).total, few_layout(T, V, D, h, w, true).total);
+  return grad_bytes(T, V, D, want_dhidden != 0, want_dweight != 0, false);
+}
+extern "C" int64_t simple_xent_grad_workspace_aligned(int64_t T, int64_t V, int64_t D, int want_dhidden, int want_dweight) {
+  const int rc = check_sizes(T, V, D);
+  if (rc != SIMPLE_OK) return rc;
+  return grad_bytes(T, V, D, want_dhidden != 0, want_dweight != 0, true);
 }
 
 extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, int64_t hidden_stride, const void* weight_dev, int64_t weight_stride,
@@ -916,10 +937,13 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   if (T == 0) dhidden_dev = nullptr;
   if (!dhidden_dev && (!dweight_dev || (T == 0 && accumulate))) return SIMPLE_OK;
   hipStream_t st = (hipStream_t)hip_stream;
-  const Layout L = layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr);
+  const Operand all_rows{(const unsigned char*)weight_dev, weight_stride * 2, V};
+  const bool fits = direct(Operand{(const unsigned char*)hidden_dev, hidden_stride * 2, T}, D * 2) && direct(all_rows, D * 2);
+  const bool copies = !fits && T > FEW_TOKENS;
+  const Layout L = layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr, copies);
   if (T > 0) {
     if (!dloss_dev || !hidden_dev || !weight_dev || !targets_dev || !lse_dev || !workspace_dev || ((uintptr_t)workspace_dev & 15u) != 0) return SIMPLE_EINVAL;
-    if (too_many_tiles(T, V) || workspace_bytes < simple_xent_grad_workspace(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr)) return SIMPLE_ECAPACITY;
+    if (too_many_tiles(T, V) || workspace_bytes < grad_bytes(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr, fits)) return SIMPLE_ECAPACITY;
   }
   unsigned char* ws = (unsigned char*)workspace_dev;
   Args a{};
@@ -930,7 +954,6 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
   a.V = V;
   a.lse = lse_dev;
   a.dloss = dloss_dev;
-  const Operand all_rows{(const unsigned char*)weight_dev, weight_stride * 2, V};
   auto hidden = [&](const float* sums, int64_t sums_stride, int splits, const Token* tokens, const uint32_t* top) {
     auto go = [&](auto kernel, int vec) {
       const int64_t columns = (int64_t)64 * vec * (splits > 1 ? 1 : HID_GROUPS);
@@ -941,7 +964,7 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
     else go(hidden_kernel<1>, 1);
   };
   if (T > 0 && T <= FEW_GRAD) {
-    const bool fits = direct(a.hidden, D * 2) && direct(all_rows, D * 2);  // else copies with aligned rows, of the weights a piece at a time
+    // (rows that are not aligned: copies, of the weights a piece at a time)
     const FewLayout F = few_layout(T, V, D, dhidden_dev != nullptr, dweight_dev != nullptr, !fits);
     a.k_bytes = (int)(F.d_pad * 2);
     if (!fits) a.hidden = aligned_copy<2>(a.hidden, D * 2, ws + F.copy_h, st);
@@ -1007,7 +1030,6 @@ extern "C" int simple_xent_grad(const float* dloss_dev, const void* hidden_dev, 
     if (dweight_dev)
       transpose((const uint16_t*)hidden_dev, hidden_stride, T, D, (uint16_t*)(ws + L.ht), L.t16, L.t16, tokens, tops + TOP_STATES, st);
   }
-  const bool copies = T > FEW_TOKENS && !(direct(a.hidden, D * 2) && direct(Operand{weight, weight_stride * 2, V}, D * 2));
   if (copies) {
     a.hidden = aligned_copy<2>(a.hidden, D * 2, ws + L.copy_h, st);
     a.k_bytes = (int)a.hidden.stride;

@@ -21,7 +21,8 @@ from .binding import SIMPLE_BF16, SIMPLE_F32, SIMPLE_OK, SimpleError, _addresses
 
 EXPORTS = ("simple_rms_norm", "simple_rms_norm_int8", "simple_quantize_rows", "simple_rms_norm_grad", "simple_rms_norm_grad_workspace",
            "simple_embed", "simple_embed_grad", "simple_embed_grad_workspace", "simple_linear_int8", "simple_linear_int8_workspace",
-           "simple_xent", "simple_xent_workspace", "simple_xent_grad", "simple_xent_grad_workspace")
+           "simple_xent", "simple_xent_workspace", "simple_xent_workspace_aligned", "simple_xent_grad", "simple_xent_grad_workspace",
+           "simple_xent_grad_workspace_aligned")
 
 
 def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
@@ -39,8 +40,10 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
         "simple_linear_int8_workspace": (i64, i64, i64, i64),
         "simple_xent": (ci, vp, i64, vp, i64, vp, i64, i64, i64, f32, vp, vp, vp, i64, vp),
         "simple_xent_workspace": (i64, i64, i64, i64),
+        "simple_xent_workspace_aligned": (i64, i64, i64, i64),
         "simple_xent_grad": (ci, vp, vp, i64, vp, i64, vp, vp, i64, i64, i64, f32, vp, i64, vp, i64, ci, ci, vp, i64, vp),
         "simple_xent_grad_workspace": (i64, i64, i64, i64, ci, ci),
+        "simple_xent_grad_workspace_aligned": (i64, i64, i64, i64, ci, ci),
     }
     assert set(signatures) == set(EXPORTS)
     for name, (restype, *argtypes) in signatures.items():
@@ -257,13 +260,20 @@ def _xent_inputs(hidden, weight, targets):
     return T, V, D
 
 
+def _aligned(hidden, weight) -> bool:
+    """Whether the rows of both start at multiples of 16 bytes and are as long, so that a call has no copies of them."""
+    h, w = _stride(hidden), _stride(weight)
+    return (hidden.data_ptr() | weight.data_ptr()) % 16 == 0 and (h | w | hidden.shape[1]) % 8 == 0 and max(h, w) <= 1 << 21
+
+
 def linear_xent(hidden, weight, targets, *, logit_scale: float = 1.0, loss=None, lse=None):
     """``(loss, lse)``, float32 [T]: negative log-probability of ``targets`` (int32; outside the vocabulary: 0) under the logits
     ``logit_scale * hidden @ weight.T``, and the logarithm of the sum of their exponentials.  bfloat16 operands."""
     T, V, D = _xent_inputs(hidden, weight, targets)
     loss = _out(loss, "loss", (T,), torch.float32, hidden.device)
     lse = _out(lse, "lse", (T,), torch.float32, hidden.device)
-    ws = _workspace(_lib.simple_xent_workspace(T, V, D), "simple_xent_workspace", hidden.device)
+    size = _lib.simple_xent_workspace_aligned if _aligned(hidden, weight) else _lib.simple_xent_workspace
+    ws = _workspace(size(T, V, D), "simple_xent_workspace", hidden.device)
     _check(_lib.simple_xent(hidden.data_ptr(), _stride(hidden), weight.data_ptr(), _stride(weight), targets.data_ptr(), T, V, D, logit_scale,
                             loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), _current_stream()), "simple_xent")
     return loss, lse
@@ -286,7 +296,8 @@ def linear_xent_grad(dloss, hidden, weight, targets, lse, *, logit_scale: float 
     else:
         _dtype(dweight, "dweight")
         _out(dweight, "dweight", (V, D), dweight.dtype, hidden.device)
-    ws = _workspace(_lib.simple_xent_grad_workspace(T, V, D, int(need_dhidden), int(need_dweight)), "simple_xent_grad_workspace", hidden.device)
+    size = _lib.simple_xent_grad_workspace_aligned if _aligned(hidden, weight) else _lib.simple_xent_grad_workspace
+    ws = _workspace(size(T, V, D, int(need_dhidden), int(need_dweight)), "simple_xent_grad_workspace", hidden.device)
     _check(_lib.simple_xent_grad(dloss.data_ptr(), hidden.data_ptr(), _stride(hidden), weight.data_ptr(), _stride(weight), targets.data_ptr(),
                                  lse.data_ptr(), T, V, D, logit_scale, _ptr(dhidden), _stride(dhidden), _ptr(dweight), _stride(dweight),
                                  SIMPLE_BF16 if dweight is None else _TYPES[dweight.dtype], int(accumulate), ws.data_ptr(), ws.numel(),
