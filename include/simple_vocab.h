@@ -109,7 +109,11 @@ int64_t simple_xent_workspace_aligned(int64_t T, int64_t V, int64_t D);
 /*
  * Its gradient for a loss of sum over t of dloss[t] * loss[t]: with G[t, v] = logit_scale * dloss[t] * (exp(z[t, v] - lse[t]) - [v = targets[t]]),
  *   dhidden = G * weight (bfloat16),   dweight = transposed G * hidden (dweight_dtype; accumulate != 0 adds it to what is there)
- * lse_dev is what simple_xent wrote.  Logits are formed again, a piece of the vocabulary at a time, and G is rounded to 11 bits or more for the products.
+ * lse_dev is what simple_xent wrote.  Logits are formed again, a piece of the vocabulary at a time, and G is rounded for the products: of up to 64
+ * tokens to 16 bits at any size; of more to 11 bits down to 2^-28 of the token's largest element (1 - p at its target), and to steps of 2^-38 of that
+ * below, so that a row of weight which is less probable under every token gets a row of zeros.  For dweight the states of more than 64 tokens, times logit_scale, dloss and 1 - p
+ * of their token, are rounded likewise, to 11 bits down to 2^-28 of the largest of all tokens (which should be above 2^-60); for dhidden
+ * weights are exact down to 2^-28 of the largest.
  * A token whose target is outside [0, V) or whose dloss is 0 takes no part whatever its states hold: its row of dhidden is zeros.
  * Either output may be NULL: then it is not formed.  workspace_dev: simple_xent_grad_workspace() bytes for the outputs wanted, 16-byte aligned
  * (simple_xent_grad_workspace_aligned() where the rows of hidden and weight are, as above).
