@@ -803,13 +803,16 @@ void transpose(const uint16_t* in, int64_t stride, int64_t rows, int64_t cols, u
     hipLaunchKernelGGL(transpose_kernel<false>, grid, dim3(256), 0, st, in, stride, rows, cols, out, out_stride, r_out, tokens, top);
 }
 
+// Few steps of k, as dW of few tokens has: a tile is mostly stored, and two smaller ones on a compute unit do so in turn.  So too where a tile of 256
+// columns would be half empty.
+int multiply_tiles(int64_t p, int64_t q, int64_t k_bytes, int splits) {
+  const int tiles = tiles_for(p, q);
+  return k_bytes <= SHORT_K || q <= 128 ? std::min<int>(tiles, TILE_128) : splits > 1 && p > 128 ? TILE_256 : tiles;
+}
 void multiply(MulArgs a, int type, bool add, int splits, hipStream_t st) {
   a.k_split = (int)(ceil_div(ceil_div(a.k_bytes, splits), KB) * KB);
   a.vec = rows_aligned(a.out, a.stride, type_bytes(type), 16);
-  // (Few steps of k, as dW of few tokens has: a tile is mostly stored, and two smaller ones on a compute unit do so in turn.)
-  // (So too where a tile of 256 columns would be half empty.)
-  const int tiles = tiles_for(a.p.rows, a.q.rows);
-  shaped<F16>(a.k_bytes <= SHORT_K || a.q.rows <= 128 ? std::min<int>(tiles, TILE_128) : splits > 1 && a.p.rows > 128 ? TILE_256 : tiles, [&](auto shape) {
+  shaped<F16>(multiply_tiles(a.p.rows, a.q.rows, a.k_bytes, splits), [&](auto shape) {
     using S = decltype(shape);
     a.plan = plan<S, Cut<S>::CAN>(a.p.rows, a.q.rows, splits == 1);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)a.plan.grid, (unsigned)splits), dim3(S::THREADS), 0, st, a); };
