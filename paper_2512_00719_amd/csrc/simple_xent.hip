@@ -665,7 +665,6 @@ __global__ __launch_bounds__(256) void dw_few_kernel(const uint16_t* gt, int64_t
       }
     }
   const int64_t d_end = min(D, ((int64_t)blockIdx.y + 1) * FEW_COLUMNS);
-#pragma unroll 2
   for (int64_t d0 = (int64_t)blockIdx.y * FEW_COLUMNS; d0 < d_end; d0 += 32) {
     i32x4 h[2][KS];
 #pragma unroll
