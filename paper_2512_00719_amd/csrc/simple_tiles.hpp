@@ -55,7 +55,7 @@ __device__ __forceinline__ void to_lds(uint32_t lds, uint32_t offset, i32x4 reso
   k = (uint32_t)__builtin_amdgcn_readfirstlane((int)k);
   resource = i32x4{__builtin_amdgcn_readfirstlane(resource.x), __builtin_amdgcn_readfirstlane(resource.y), __builtin_amdgcn_readfirstlane(resource.z),
                    __builtin_amdgcn_readfirstlane(resource.w)};
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(resource), "s"(k) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(resource), "s"(k) : "memory");
 }
 // All but the `N` newest of this wave's loads have arrived, and those of the workgroup's other waves; what the waves read of LDS before is in
 // their registers.
