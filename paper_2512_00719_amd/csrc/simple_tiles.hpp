@@ -48,7 +48,8 @@ struct Operand {
 
 // ---- staging by the memory system itself: 16 bytes a lane go from memory to LDS without a register ----
 // The wave's 64 lanes write 1 KB from `lds` on in lane order: 8 rows of a step.  Nothing here is seen by the compiler's own count of loads
-// in flight; arrived() below waits for them, and no register is written.
+// in flight; arrived() below waits for them, and no register is written but m0, which the compiler keeps out of all allocation (named among the asm's it is
+// refused) and which nothing else in these kernels uses.
 __device__ __forceinline__ void to_lds(uint32_t lds, uint32_t offset, i32x4 resource, uint32_t k) {
   // (scalar operands, whatever register the optimiser has kept them in)
   lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
