@@ -1,6 +1,6 @@
 // The head in 8 bits: logits[t, v] = (sum over k of codes[t, k] * w_codes[v, k]) * scales[t] * w_scales[v], sums in 32-bit integers (exact), the
 // scales in float32, one rounding to the output's type.
-// Bound: for few tokens the weights, read once (one token, 128,256 x 4096: 93 us, 5.7 TB/s); for many the matrix rate (2048 tokens: 920 to 990 us, 2.2 to 2.3 POP/s, the
+// Bound: for few tokens the weights, read once (one token, 128,256 x 4096: 93 us, 5.7 TB/s); for many the matrix rate (2048 tokens against the same: 910 to 1010 us on different boards, 2.1 to 2.4 POP/s, the
 // 525 MB of logits written among it).
 #include "simple_tiles.hpp"
 

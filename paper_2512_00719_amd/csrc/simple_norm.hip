@@ -154,7 +154,8 @@ struct GradArgs {
 
 // A workgroup takes rows a grid apart, so that each of its threads adds up the same columns' weight gradient in registers over all of
 // them; the workgroups' sums are joined by column_sums_kernel in their order.  Bound: memory; 8192 bfloat16 rows of 4096 with dh, 268 MB, 46 us, and 5 for
-// joining 1024 workgroups' rows.
+// joining 1024 workgroups' rows.  Rows of more than 8192 values hold more than a thread's 128 registers do and spill (1024 x 16,384 162 us, 0.8 TB/s in bfloat16 and 1.65 in float32; 1024 x 8192 32
+// and 36).
 template <typename T, int VEC, bool WHOLE, int NT, int NV>
 __global__ __launch_bounds__(NT > WG ? NT : WG) void grad_kernel(GradArgs a) {
   constexpr int ROWS = NT > WG ? 1 : WG / NT;

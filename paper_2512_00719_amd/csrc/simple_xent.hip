@@ -11,7 +11,8 @@
 // (exp(z - lse) - [v = y]) has its largest magnitude, 1 - p_y, brought to 2^13 .. 2^14, so that a probability 2^-28 of it still has
 // its 11 bits (at 1 those of rare tokens, 1e-6 and below, would have had fewer than bfloat16's); the factor c dl goes with the token's states into the
 // product for dW, and behind the sum in dH; states and weights are brought below 2^14 by their largest magnitude.  Weights are then
-// exact (8 bits within 28 binades of the largest), G and the states rounded once, to 2^-12.  dH is summed over the pieces in float32.
+// exact (8 bits within 28 binades of the largest), G and the states (the factor is no power of two) rounded once, to 11 bits; what is smaller than 2^-28 of its
+// row's largest, or of all tokens' states', loses bits, and below 2^-39 is zero.  dH is summed over the pieces in float32.
 // Tokens whose target is outside the vocabulary or whose dl is 0 take no part: their states are read as zeros where sums over tokens are
 // formed, so that a NaN in them stays with them.
 #include <algorithm>
@@ -108,7 +109,7 @@ __device__ __forceinline__ void stats_of(const Args& a, typename S::Acc (&acc)[S
     a.pairs[q0 / S::BQ * T + p0 + t] = v;
   }
 }
-// 8192 tokens against 128,256 x 4096 6.05 to 6.4 ms (1.34 to 1.42 PFLOP/s); 16 tokens 169 us (1.05 GB of weights, 6.2 TB/s).
+// 8192 tokens against 128,256 x 4096 6.05 to 6.4 ms (1.34 to 1.42 PFLOP/s, by the board); 16 tokens 169 us (1.05 GB of weights, 6.2 TB/s).
 template <class S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void stats_kernel(Args a) {
   __shared__ __align__(1024) unsigned char lds[S::LDS + stats_room<S>];
@@ -539,6 +540,8 @@ __global__ __launch_bounds__(64 * HID_GROUPS) void hidden_kernel(const float* su
 // ---- few tokens: the weights are what is read, and each product takes them as they lie ----
 // G is the sum of two bfloat16 values, 16 bits that need no range, so that neither weights nor states are copied into another type; twice the matrix
 // instructions are free where the memory is the bound.
+// Both outputs of 64 tokens against 128,256 x 4096, 50,001 x 1024 and 33,858 x 1408: 1017, 111 and 106 us so, 1407, 153 and 154 the other way (of 16 tokens 753, 85 and 77; 1378, 143
+// and 147); 65 tokens, the other way, 1454, 162 and 160.  The bound is where this way's fragments in registers end, not where it stops paying.
 constexpr int64_t FEW_GRAD = 64;
 constexpr int FEW_STAGES = 3, FEW_K = 64;  // rows of the weights a step
 
